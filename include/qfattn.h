@@ -18,8 +18,11 @@
  * around them (qf_attn_combine_current folds in the current token, qf_kv_append writes it to the
  * cache, qf_attn_combine_current_append does both in one launch); the dense products of a decoder block
  * (qf_linear, qf_linear_pair) and the sweep sharing one launch with
- * one of them (qf_attn_decode_split_beside); and a host-side simulation of the layer-wise decode
- * schedule (qf_schedule_simulate).
+ * one of them (qf_attn_decode_split_beside); what brings prompts into the cache and reads what requests
+ * share in it (qf_qkv_rope_append: norm, rotation and append of any number of new tokens;
+ * qf_attn_prefill: their causal attention; qf_attn_decode_shared: decode attention over prefixes that
+ * requests share); and a host-side simulation of the layer-wise decode schedule
+ * (qf_schedule_simulate).
  *
  * Conventions shared by every entry point
  *   - Every pointer argument except `stream` is a DEVICE pointer, owned by the caller, except
@@ -48,7 +51,7 @@
 extern "C" {
 #endif
 
-#define QF_VERSION 10
+#define QF_VERSION 11
 
 #define QF_OK 0
 #define QF_EINVAL (-1)       /* null pointer, negative or inconsistent size, Hq % Hkv != 0   */
@@ -443,6 +446,116 @@ int qf_attn_decode_split_beside(const qf_decode_desc* desc, const void* q, const
                                 float* part_out, float* part_lse, void* workspace,
                                 size_t workspace_size, const qf_linear_args* beside,
                                 void* stream);
+
+/*
+ * New tokens on their way into attention, any number per request: queries and keys normalised per head
+ * and rotated by their positions, keys and values written into the paged cache.  Tokens are packed:
+ * request b has rows cu_tokens[b] .. cu_tokens[b + 1] - 1, and its i-th row is the token at position
+ * p = ctx_lens[b] + i.  For every head of a row,
+ *
+ *     n(x) = x / sqrt(mean_i x_i^2 + eps) * gain      (x itself where the gain is NULL)
+ *     (x0, x1) -> amplitude * (x0 cos(p f_i) - x1 sin(p f_i), x1 cos(p f_i) + x0 sin(p f_i)),
+ *
+ * f_i = freqs[i], over the pairs of dims (i, i + rotary_dim / 2) (QF_ROPE_HALF) or (2i, 2i + 1)
+ * (QF_ROPE_INTERLEAVED), i < rotary_dim / 2; dims from rotary_dim on pass.  Extended contexts are a matter
+ * of the frequencies and the amplitude.  The angle is computed and reduced in fp64, the rest in fp32,
+ * with one rounding per output.
+ *
+ *   desc        batch, n_q_heads, n_kv_heads, head_dim, page_size, max_pages_per_seq and num_pages are
+ *               used (the other fields have to be valid).
+ *   n_tokens    rows of q, k, v and q_out, >= 0.  Rows that lie in no request are left as they are.
+ *   cu_tokens   int32 [batch + 1], not decreasing, in [0, n_tokens]; NULL: one token per request (a
+ *               decode step; n_tokens == batch).  Values out of order or range never cause an
+ *               out-of-bounds access; rows of such a request may be skipped.
+ *   ctx_lens    int32 [batch]: positions cached before these tokens.  It is not advanced (the calls of
+ *               the other layers read it too).
+ *   rope        HOST pointer, read during the call; NULL: no rotation.  freqs: DEVICE pointer, fp64
+ *               [rotary_dim / 2], radians per position, 8-byte aligned; rotary_dim a multiple of 16 in
+ *               [0, head_dim]; amplitude finite.
+ *   q, k, v     bf16, 16-byte aligned: row t's heads are [n_q_heads or n_kv_heads, head_dim] at
+ *               t * stride elements (strides: multiples of 8, at least the row's elements), so that
+ *               they can be columns of one product.  q NULL: no queries (q_out is not used); k and v
+ *               both NULL: nothing is appended.
+ *   q_gain, k_gain   bf16 [head_dim], 16-byte aligned, or NULL.
+ *   q_out       bf16 [n_tokens, Hq, D], 16-byte aligned; may be q itself (with q_stride Hq * D), and
+ *               must not overlap the inputs otherwise.
+ *   k_cache, v_cache   bf16 [num_pages, Hkv, P, D], 16-byte aligned, written in place.
+ *   status      optional int32 device word: set to 1 (never cleared) when a token is not appended
+ *               because its position is past the table or its page outside the pool.
+ */
+#define QF_ROPE_HALF 0
+#define QF_ROPE_INTERLEAVED 1
+typedef struct qf_rope {
+  int32_t rotary_dim;
+  int32_t layout;
+  const double* freqs;
+  float amplitude;
+} qf_rope;
+int qf_qkv_rope_append(const qf_decode_desc* desc, int32_t n_tokens, const int32_t* cu_tokens,
+                       const int32_t* ctx_lens, const qf_rope* rope, const void* q, int64_t q_stride,
+                       const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                       const void* q_gain, const void* k_gain, float eps, void* q_out, void* k_cache,
+                       void* v_cache, const int32_t* block_table, int32_t* status, void* stream);
+
+/*
+ * Causal attention of packed new tokens over the paged cache, for whole prompts, chunks of them, or a
+ * few tokens at the end of a long context: row i of request b (cu_tokens as for qf_qkv_rope_append)
+ * sees positions 0 .. ctx_lens[b] + i, all of which are in the cache already, its own included
+ * (qf_qkv_rope_append with the same ctx_lens puts them there):
+ *
+ *     out = sum_{j <= ctx + i} exp(s_j) v_j / Z,   s_j = softmax_scale q . k_j,   lse = ln Z.
+ *
+ * What a row does not see never reaches it, infinities and NaN included.
+ *
+ *   desc        every field but max_shards (which has to be valid).
+ *   q           bf16 [n_tokens, Hq, D], 16-byte aligned.
+ *   k_cache, v_cache, block_table   as for qf_attn_decode_split.
+ *   ctx_lens    int32 [batch], with ctx_lens[b] + its tokens <= max_pages_per_seq * P; otherwise the
+ *               request's out and lse are NaN.  A page outside the pool makes NaN of the rows that see it.
+ *   cu_tokens   int32 [batch + 1], not decreasing, in [0, n_tokens].  Rows that lie in no request are
+ *               left as they are.
+ *   out         bf16 [n_tokens, Hq, D], 8-byte aligned; lse fp32 [n_tokens, Hq] natural log, or NULL.
+ *               Neither may overlap the inputs.
+ *   workspace   at least qf_attn_prefill_workspace_size() bytes, 16-byte aligned; may be NULL when that
+ *               is 0.  It holds the pairs of key ranges where there are few rows; no initialisation
+ *               needed.  Calls that may run at the same time need workspaces of their own.
+ * The weights are rounded to bf16 for the product with V (their sum is not); everything else is fp32.
+ */
+int qf_attn_prefill_workspace_size(const qf_decode_desc* desc, int32_t n_tokens, size_t* bytes);
+int qf_attn_prefill(const qf_decode_desc* desc, int32_t n_tokens, const void* q, const void* k_cache,
+                    const void* v_cache, const int32_t* block_table, const int32_t* ctx_lens,
+                    const int32_t* cu_tokens, void* out, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * Decode attention of one query per request where groups of consecutive requests share the beginning
+ * of their contexts: each group's prefix is swept once for all its requests, every request's own
+ * positions as by qf_attn_decode_split, and the pairs are merged (any partition gives the same
+ * attention).  Requests group_rows[i] .. group_rows[i + 1] - 1 see the prefix_lens[i] positions of
+ * row i of prefix_table, then their own ctx_lens[b] positions of block_table; requests in no group
+ * only the latter.
+ *
+ *   desc ... n_shards   as for qf_attn_decode_split (max_shards and n_shards: of a request's own
+ *               positions).  A request may have no position of its own.
+ *   n_groups    >= 0; with 0 the three arrays may be NULL.
+ *   group_rows  int32 [n_groups + 1], not decreasing, in [0, batch].
+ *   prefix_lens int32 [n_groups], 0 <= n <= max_prefix_pages * P; otherwise, and where a page lies
+ *               outside the pool, the group's out and lse are NaN.
+ *   prefix_table   int32 [n_groups, max_prefix_pages], pages of the same pools.
+ *   pair        0: out bf16 [B, Hq, D], 4-byte aligned, lse or NULL, as by qf_attn_combine.
+ *               1: out fp32 [B, 1, Hq, D], 16-byte aligned, and lse [B, 1, Hq]: the merged pair as the
+ *               one slot that qf_attn_combine_current (_append) takes with max_shards = 1.
+ *   workspace   at least qf_attn_decode_shared_workspace_size() bytes, 16-byte aligned; calls that may
+ *               run at the same time need workspaces of their own.
+ */
+int qf_attn_decode_shared_workspace_size(const qf_decode_desc* desc, int32_t n_groups,
+                                         int32_t max_prefix_pages, size_t* bytes);
+int qf_attn_decode_shared(const qf_decode_desc* desc, const void* q, const void* k_cache,
+                          const void* v_cache, int32_t n_groups, int32_t max_prefix_pages,
+                          const int32_t* prefix_table, const int32_t* prefix_lens,
+                          const int32_t* group_rows, const int32_t* block_table,
+                          const int32_t* ctx_lens, const int32_t* n_shards, int32_t pair, void* out,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Message for the last error on the calling thread; "" if none.  Valid until the thread's next
  * call into the library. */

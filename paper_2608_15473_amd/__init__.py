@@ -6,6 +6,8 @@ products of a decoder block and the sweep sharing a launch with the feed-forward
 simulation of the layer-wise decode schedule (Appendix D).  It all runs in hand-written HIP kernels
 behind the C ABI of ``include/qfattn.h`` (``lib/libqfattn.so``); this package is the thin Python
 binding over that library (``binding``) plus a stack of Q-First blocks built on it (``stage``).
+Prompts enter the cache by the norm, rotation and append of any number of tokens and their causal
+attention; prefixes that requests share are swept once for all of them.
 """
 
 from .binding import (  # noqa: F401
@@ -20,17 +22,27 @@ from .binding import (  # noqa: F401
     QF_LINEAR_RMS_NORM,
     QF_LINEAR_SWIGLU,
     QF_OK,
+    QF_ROPE_HALF,
+    QF_ROPE_INTERLEAVED,
     DecodeDesc,
     LinearArgs,
+    PrefillPlan,
     QFError,
+    Rope,
+    RopeAppendPlan,
+    SharedDecodePlan,
     attn_combine,
     attn_combine_current,
     attn_combine_current_append,
     attn_decode,
     attn_decode_noalloc,
+    attn_decode_shared,
+    attn_decode_shared_workspace_size,
     attn_decode_split,
     attn_decode_split_beside,
     attn_decode_split_unfolded,
+    attn_prefill,
+    attn_prefill_workspace_size,
     split_chunks,
     DecodeStepPlan,
     decode_workspace_size,
@@ -42,5 +54,7 @@ from .binding import (  # noqa: F401
     linear_attn_current,
     linear_beside_merge,
     linear_pair,
+    qkv_rope_append,
+    rope_frequencies,
     workspace_size,
 )

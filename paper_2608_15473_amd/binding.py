@@ -8,6 +8,7 @@ There is no fallback: if the library is missing or the tensors are not on a GPU,
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -21,7 +22,10 @@ EXPORTED = ("qf_attn_decode_split_workspace_size", "qf_attn_decode_split", "qf_a
             "qf_attn_decode_workspace_size", "qf_attn_decode", "qf_attn_decode_noalloc",
             "qf_attn_combine_current", "qf_attn_combine_current_append", "qf_kv_append",
             "qf_linear", "qf_linear_pair", "qf_linear_beside_merge", "qf_linear_attn_current",
-            "qf_attn_decode_split_beside", "qf_schedule_simulate", "qf_last_error", "qf_version")
+            "qf_attn_decode_split_beside", "qf_qkv_rope_append", "qf_attn_prefill_workspace_size",
+            "qf_attn_prefill", "qf_attn_decode_shared_workspace_size", "qf_attn_decode_shared",
+            "qf_schedule_simulate", "qf_last_error", "qf_version")
+QF_ROPE_HALF, QF_ROPE_INTERLEAVED = 0, 1
 QF_WIRING_QFIRST, QF_WIRING_COMPOSED = 0, 1
 QF_LINEAR_PLAIN, QF_LINEAR_RMS_NORM, QF_LINEAR_SWIGLU, QF_LINEAR_GLU_OUT = 0, 1, 2, 16
 
@@ -45,6 +49,11 @@ class LinearArgs(ctypes.Structure):
                 ("prologue", ctypes.c_int32), ("x", ctypes.c_void_p), ("w", ctypes.c_void_p),
                 ("gain", ctypes.c_void_p), ("eps", ctypes.c_float), ("residual", ctypes.c_void_p),
                 ("out", ctypes.c_void_p), ("n_split", ctypes.c_int32), ("out_b", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("freqs", ctypes.c_void_p), ("amplitude", ctypes.c_float)]
 
 
 _lib = None
@@ -88,6 +97,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                            vp, vp, vp, vp, ctypes.POINTER(LinearArgs), vp]
     lib.qf_attn_decode_split_beside.argtypes = [ctypes.POINTER(DecodeDesc), vp, vp, vp, vp, vp, vp,
                                                 vp, vp, vp, sz, ctypes.POINTER(LinearArgs), vp]
+    i64 = ctypes.c_int64
+    lib.qf_qkv_rope_append.argtypes = [ctypes.POINTER(DecodeDesc), i32, vp, vp, ctypes.POINTER(Rope),
+                                       vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp,
+                                       vp, vp, vp]
+    lib.qf_attn_prefill_workspace_size.argtypes = [ctypes.POINTER(DecodeDesc), i32, ctypes.POINTER(sz)]
+    lib.qf_attn_prefill.argtypes = [ctypes.POINTER(DecodeDesc), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                    sz, vp]
+    lib.qf_attn_decode_shared_workspace_size.argtypes = [ctypes.POINTER(DecodeDesc), i32, i32,
+                                                         ctypes.POINTER(sz)]
+    lib.qf_attn_decode_shared.argtypes = [ctypes.POINTER(DecodeDesc), vp, vp, vp, i32, i32, vp, vp, vp,
+                                          vp, vp, vp, i32, vp, vp, vp, sz, vp]
     dp = ctypes.POINTER(ctypes.c_double)
     lib.qf_schedule_simulate.argtypes = [i32, dp, dp, i32, i32, ctypes.c_double, i32,
                                          ctypes.c_double, dp, dp, dp, dp, dp]
@@ -100,7 +120,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                  "qf_attn_combine", "qf_attn_combine_current", "qf_attn_combine_current_append",
                  "qf_kv_append",
                  "qf_linear", "qf_linear_pair", "qf_linear_beside_merge", "qf_linear_attn_current",
-                 "qf_attn_decode_split_beside", "qf_schedule_simulate", "qf_version"):
+                 "qf_attn_decode_split_beside", "qf_qkv_rope_append",
+                 "qf_attn_prefill_workspace_size", "qf_attn_prefill",
+                 "qf_attn_decode_shared_workspace_size", "qf_attn_decode_shared",
+                 "qf_schedule_simulate", "qf_version"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -656,6 +679,317 @@ def attn_decode_noalloc(q, k_cache, v_cache, block_table, ctx_lens, n_shards, ma
         ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
         _ptr(ctx_lens), _ptr(n_shards), _ptr(out), _ptr(lse), ctypes.c_void_p(stream)))
     return out, lse
+
+
+def _heads_of(t, name, tokens=None):
+    """Rows of heads [tokens, heads, D] whose rows may be columns of a wider product; returns the
+    rows' stride in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise QFError(QF_EINVAL, f"{name} must be a GPU tensor (got {t.device})")
+    if t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise QFError(QF_EINVAL, f"{name} must be bfloat16 [tokens, heads, D]")
+    if tokens is not None and t.shape[0] != tokens:
+        raise QFError(QF_EINVAL, f"{name} has {t.shape[0]} tokens, not {tokens}")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise QFError(QF_EINVAL, f"the heads of a row of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise QFError(QF_EINVAL, f"{name} is on {t.device}, not on {device}")
+
+
+def _cache_of(k_cache, v_cache, block_table, ctx_lens):
+    """Checks of a paged cache and its indexes; returns (batch, Hkv, P, D)."""
+    _require(k_cache, "k_cache", torch.bfloat16, 4)
+    _require(v_cache, "v_cache", torch.bfloat16, 4)
+    if v_cache.shape != k_cache.shape:
+        raise QFError(QF_EINVAL, "k_cache and v_cache shapes differ")
+    _require(ctx_lens, "ctx_lens", torch.int32, 1)
+    B = ctx_lens.shape[0]
+    if block_table is not None:
+        _require(block_table, "block_table", torch.int32, 2)
+        if block_table.shape[0] != B:
+            raise QFError(QF_EINVAL, f"block_table has {block_table.shape[0]} rows for {B} requests")
+    return (B, *k_cache.shape[1:])
+
+
+class _Plan:
+    """One library call with its arguments checked and converted once; see the subclasses."""
+
+    def _bind(self, device, stream, function, args, keep):
+        if stream is None:
+            stream = torch.cuda.current_stream(device).cuda_stream
+        self._device, self._function = device, function
+        self._args = args + (ctypes.c_void_p(stream),)
+        self._keep = keep
+
+    def _call(self):
+        # The library launches on the current device, which is the stream's.
+        if torch.cuda.current_device() == self._device.index:
+            rc = self._function(*self._args)
+        else:
+            with torch.cuda.device(self._device):
+                rc = self._function(*self._args)
+        if rc != QF_OK:
+            raise QFError(rc, load_library().qf_last_error().decode())
+
+
+_ROPE_LAYOUTS = {"half": QF_ROPE_HALF, "interleaved": QF_ROPE_INTERLEAVED}
+
+
+class RopeAppendPlan(_Plan):
+    """``qkv_rope_append`` on fixed buffers, checked and converted once: the arguments are those of
+    ``qkv_rope_append``; calling the plan enqueues the library call on ``stream`` (default: the
+    current stream at construction) with the pointers taken at construction, and returns q_out."""
+
+    def __init__(self, q, k, v, k_cache, v_cache, block_table, ctx_lens, cu_tokens=None, freqs=None,
+                 layout="half", amplitude=1.0, q_gain=None, k_gain=None, eps=1e-6, q_out=None,
+                 status=None, max_pages=None, stream=None):
+        if (k is None) != (v is None):
+            raise QFError(QF_EINVAL, "k and v go together")
+        if q is None and k is None:
+            raise QFError(QF_EINVAL, "neither queries nor keys are given")
+        some = q if q is not None else k
+        if not isinstance(some, torch.Tensor) or some.dim() != 3:
+            raise QFError(QF_EINVAL, "q and k must be tensors [tokens, heads, D]")
+        T, _, D = some.shape
+        strides = [0 if t is None else _heads_of(t, name, T) for t, name in ((q, "q"), (k, "k"), (v, "v"))]
+        if k is not None:
+            B, Hkv, P, Dc = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+            if tuple(k.shape) != (T, Hkv, Dc) or tuple(v.shape) != (T, Hkv, Dc):
+                raise QFError(QF_EINVAL, "k and v do not match the cache")
+            if max_pages is None:
+                max_pages = block_table.shape[1] if block_table is not None else k_cache.shape[0] // max(B, 1)
+            num_pages = k_cache.shape[0]
+        else:
+            _require(ctx_lens, "ctx_lens", torch.int32, 1)
+            B, Hkv, P, max_pages, num_pages = ctx_lens.shape[0], q.shape[1], 16, 1, 1
+        if cu_tokens is not None:
+            _require(cu_tokens, "cu_tokens", torch.int32, 1)
+            if cu_tokens.shape[0] != B + 1:
+                raise QFError(QF_EINVAL, f"cu_tokens must have {B + 1} entries")
+        if layout not in _ROPE_LAYOUTS:
+            raise QFError(QF_EINVAL, f"unknown rope layout {layout!r}")
+        if freqs is not None:
+            _require(freqs, "freqs", torch.float64, 1)
+        for g, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+            if g is not None:
+                _require(g, name, torch.bfloat16, 1)
+                if g.shape[0] != D:
+                    raise QFError(QF_EINVAL, f"{name} must have {D} entries")
+        if status is not None:
+            _require(status, "status", torch.int32)
+        Hq = q.shape[1] if q is not None else Hkv
+        if q is not None:
+            if q.shape[2] != D:
+                raise QFError(QF_EINVAL, "q and k have different head dimensions")
+            if q_out is None:
+                q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+            _require(q_out, "q_out", torch.bfloat16, 3)
+            if q_out.shape != q.shape:
+                raise QFError(QF_EINVAL, "q_out must have q's shape")
+        _same_device(some.device, q=q, k=k, v=v, k_cache=k_cache if k is not None else None,
+                     v_cache=v_cache if k is not None else None, block_table=block_table,
+                     ctx_lens=ctx_lens, cu_tokens=cu_tokens, freqs=freqs, q_gain=q_gain, k_gain=k_gain,
+                     q_out=q_out, status=status)
+        desc = DecodeDesc(B, Hq, Hkv, D, P, int(max_pages), int(num_pages), 1, 1.0)
+        rope = None if freqs is None else Rope(2 * freqs.shape[0], _ROPE_LAYOUTS[layout],
+                                               freqs.data_ptr(), float(amplitude))
+        self.q_out = q_out if q is not None else None
+        args = (ctypes.byref(desc), T, _ptr(cu_tokens), _ptr(ctx_lens),
+                None if rope is None else ctypes.byref(rope), _ptr(q), strides[0], _ptr(k), strides[1],
+                _ptr(v), strides[2], _ptr(q_gain), _ptr(k_gain), float(eps), _ptr(self.q_out),
+                _ptr(k_cache if k is not None else None), _ptr(v_cache if k is not None else None),
+                _ptr(block_table), _ptr(status))
+        self._bind(some.device, stream, load_library().qf_qkv_rope_append, args,
+                   (desc, rope, q, k, v, k_cache, v_cache, block_table, ctx_lens, cu_tokens, freqs,
+                    q_gain, k_gain, q_out, status))
+
+    def __call__(self):
+        self._call()
+        return self.q_out
+
+
+def qkv_rope_append(q, k, v, k_cache, v_cache, block_table, ctx_lens, cu_tokens=None, freqs=None,
+                    layout="half", amplitude=1.0, q_gain=None, k_gain=None, eps=1e-6, q_out=None,
+                    status=None, max_pages=None):
+    """Packed new tokens: q and k normalised per head and rotated, k and v written into the cache
+    (qf_qkv_rope_append).
+
+    q bf16 [T, Hq, D], k / v bf16 [T, Hkv, D] (rows may be columns of one wider product); q None
+    (keys and values only) or k and v None (queries only; the caches are not used).  cu_tokens int32
+    [B + 1]: request b's tokens are rows cu_tokens[b] .. cu_tokens[b + 1] - 1, at positions
+    ctx_lens[b], ctx_lens[b] + 1, ...; None: one token per request.  freqs fp64 [rotary_dim / 2]
+    radians per position (``rope_frequencies``), None for no rotation; q_gain / k_gain bf16 [D], None
+    for no norm.  ctx_lens is not advanced.  Returns q_out bf16 [T, Hq, D] (may be given as q itself)."""
+    return RopeAppendPlan(q, k, v, k_cache, v_cache, block_table, ctx_lens, cu_tokens, freqs, layout,
+                          amplitude, q_gain, k_gain, eps, q_out, status, max_pages)()
+
+
+def rope_frequencies(rotary_dim, theta=1e6, stretch=1.0, trained=None, device=None):
+    """Radians per position of the rotary_dim / 2 pairs, fp64 on ``device``: theta^(-2i / rotary_dim),
+    for a context extended ``stretch`` times divided by it.  With ``trained``, the context length of the
+    training, only the pairs that turn less than once in it are divided by the whole factor, those that
+    turn 32 times or more keep their frequency, and between the two the factor's share falls linearly
+    with the turns."""
+    if rotary_dim < 0 or rotary_dim % 2 or not theta > 0 or not stretch > 0:
+        raise QFError(QF_EINVAL, "need an even rotary_dim >= 0, theta > 0 and stretch > 0")
+    f = float(theta) ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / max(rotary_dim, 1))
+    share = torch.ones_like(f)
+    if trained is not None:
+        share = 1.0 - ((f * (trained / (2 * math.pi)) - 1.0) / 31.0).clamp(0.0, 1.0)
+    return (f * (1.0 - share) + f / stretch * share).to(device)
+
+
+def attn_prefill_workspace_size(desc: DecodeDesc, n_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().qf_attn_prefill_workspace_size(ctypes.byref(desc), n_tokens, ctypes.byref(n)))
+    return n.value
+
+
+def _outputs(q, out, lse, want_lse, dtype=torch.bfloat16, shape=None):
+    """Allocates or checks the attention and log-sum-exp of q [rows, Hq, D]."""
+    shape = tuple(q.shape) if shape is None else shape
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(shape[:-1], dtype=torch.float32, device=q.device)
+    _require(out, "out", dtype)
+    if lse is not None:
+        _require(lse, "lse", torch.float32)
+    if tuple(out.shape) != shape or (lse is not None and tuple(lse.shape) != shape[:-1]):
+        raise QFError(QF_EINVAL, f"out / lse must be {list(shape)} and {list(shape[:-1])}")
+    return out, lse
+
+
+def _workspace(need, given, device):
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _require(given, "workspace", torch.uint8)
+    return given
+
+
+class PrefillPlan(_Plan):
+    """``attn_prefill`` on fixed buffers, checked and converted once (arguments of ``attn_prefill``);
+    calling the plan enqueues the library call on ``stream`` (default: the current stream at
+    construction) with the pointers taken at construction, and returns (out, lse)."""
+
+    def __init__(self, q, k_cache, v_cache, block_table, ctx_lens, cu_tokens, scale=None, out=None,
+                 lse=None, workspace=None, max_pages=None, want_lse=True, stream=None):
+        _require(q, "q", torch.bfloat16, 3)
+        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+        _require(cu_tokens, "cu_tokens", torch.int32, 1)
+        if cu_tokens.shape[0] != B + 1:
+            raise QFError(QF_EINVAL, f"cu_tokens must have {B + 1} entries")
+        if q.shape[2] != D:
+            raise QFError(QF_EINVAL, "q and the cache have different head dimensions")
+        desc = make_desc(q, k_cache, block_table, 1, D ** -0.5 if scale is None else scale,
+                         max_pages=max_pages if max_pages is not None or block_table is not None
+                         else k_cache.shape[0] // max(B, 1))
+        desc.batch = B
+        out, lse = _outputs(q, out, lse, want_lse)
+        workspace = _workspace(attn_prefill_workspace_size(desc, q.shape[0]), workspace, q.device)
+        _same_device(q.device, k_cache=k_cache, v_cache=v_cache, block_table=block_table,
+                     ctx_lens=ctx_lens, cu_tokens=cu_tokens, out=out, lse=lse, workspace=workspace)
+        self.out, self.lse = out, lse
+        args = (ctypes.byref(desc), q.shape[0], _ptr(q), _ptr(k_cache), _ptr(v_cache),
+                _ptr(block_table), _ptr(ctx_lens), _ptr(cu_tokens), _ptr(out), _ptr(lse),
+                _ptr(workspace), 0 if workspace is None else workspace.numel())
+        self._bind(q.device, stream, load_library().qf_attn_prefill, args,
+                   (desc, q, k_cache, v_cache, block_table, ctx_lens, cu_tokens, out, lse, workspace))
+
+    def __call__(self):
+        self._call()
+        return self.out, self.lse
+
+
+def attn_prefill(q, k_cache, v_cache, block_table, ctx_lens, cu_tokens, scale=None, out=None, lse=None,
+                 workspace=None, max_pages=None, want_lse=True):
+    """Causal attention of packed new tokens over the paged cache (qf_attn_prefill).
+
+    q bf16 [T, Hq, D]; request b's tokens are rows cu_tokens[b] .. cu_tokens[b + 1] - 1 (int32
+    [B + 1]), the i-th of which sees positions 0 .. ctx_lens[b] + i: their keys and values are in the
+    cache already (``qkv_rope_append``).  Rows of no request are left as they are.  Returns (out bf16
+    [T, Hq, D], lse fp32 [T, Hq])."""
+    return PrefillPlan(q, k_cache, v_cache, block_table, ctx_lens, cu_tokens, scale, out, lse, workspace,
+                       max_pages, want_lse)()
+
+
+def attn_decode_shared_workspace_size(desc: DecodeDesc, n_groups: int, max_prefix_pages: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().qf_attn_decode_shared_workspace_size(ctypes.byref(desc), n_groups,
+                                                               max_prefix_pages, ctypes.byref(n)))
+    return n.value
+
+
+class SharedDecodePlan(_Plan):
+    """``attn_decode_shared`` on fixed buffers, checked and converted once (arguments of
+    ``attn_decode_shared``); calling the plan enqueues the library call on ``stream`` (default: the
+    current stream at construction) with the pointers taken at construction, and returns (out, lse)."""
+
+    def __init__(self, q, k_cache, v_cache, prefix_table, prefix_lens, group_rows, block_table, ctx_lens,
+                 n_shards, max_shards=None, scale=None, out=None, lse=None, workspace=None,
+                 max_pages=None, want_lse=True, pair=False, stream=None):
+        _require(q, "q", torch.bfloat16, 3)
+        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+        if q.shape[0] != B or q.shape[2] != D:
+            raise QFError(QF_EINVAL, "q does not match ctx_lens and the cache")
+        _require(prefix_table, "prefix_table", torch.int32, 2)
+        _require(prefix_lens, "prefix_lens", torch.int32, 1)
+        _require(group_rows, "group_rows", torch.int32, 1)
+        NG, pages = prefix_table.shape
+        if prefix_lens.shape[0] != NG or group_rows.shape[0] != NG + 1:
+            raise QFError(QF_EINVAL, f"{NG} groups need as many prefix_lens and {NG + 1} group_rows")
+        if isinstance(n_shards, int):
+            if max_shards is None:
+                max_shards = n_shards
+            n_shards = torch.full((B,), n_shards, dtype=torch.int32, device=q.device)
+        _require(n_shards, "n_shards", torch.int32, 1)
+        if n_shards.shape[0] != B:
+            raise QFError(QF_EINVAL, f"n_shards must have {B} entries")
+        if max_shards is None:
+            raise QFError(QF_EINVAL, "max_shards is required when n_shards is a tensor")
+        desc = make_desc(q, k_cache, block_table, max_shards, D ** -0.5 if scale is None else scale,
+                         max_pages=max_pages)
+        out, lse = _outputs(q, out, lse, want_lse or pair, torch.float32 if pair else torch.bfloat16,
+                            (B, 1, *q.shape[1:]) if pair else None)
+        workspace = _workspace(attn_decode_shared_workspace_size(desc, NG, pages), workspace, q.device)
+        _same_device(q.device, k_cache=k_cache, v_cache=v_cache, prefix_table=prefix_table,
+                     prefix_lens=prefix_lens, group_rows=group_rows, block_table=block_table,
+                     ctx_lens=ctx_lens, n_shards=n_shards, out=out, lse=lse, workspace=workspace)
+        self.out, self.lse = out, lse
+        args = (ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), NG, pages,
+                _ptr(prefix_table), _ptr(prefix_lens), _ptr(group_rows), _ptr(block_table),
+                _ptr(ctx_lens), _ptr(n_shards), 1 if pair else 0, _ptr(out), _ptr(lse),
+                _ptr(workspace), 0 if workspace is None else workspace.numel())
+        self._bind(q.device, stream, load_library().qf_attn_decode_shared, args,
+                   (desc, q, k_cache, v_cache, prefix_table, prefix_lens, group_rows, block_table,
+                    ctx_lens, n_shards, out, lse, workspace))
+
+    def __call__(self):
+        self._call()
+        return self.out, self.lse
+
+
+def attn_decode_shared(q, k_cache, v_cache, prefix_table, prefix_lens, group_rows, block_table, ctx_lens,
+                       n_shards, max_shards=None, scale=None, out=None, lse=None, workspace=None,
+                       max_pages=None, want_lse=True, pair=False):
+    """Decode attention where groups of consecutive requests share the beginning of their contexts
+    (qf_attn_decode_shared): each group's prefix is swept once for all its requests.
+
+    Requests group_rows[i] .. group_rows[i + 1] - 1 (int32 [groups + 1]) see the prefix_lens[i]
+    positions of the pages prefix_table[i] (int32 [groups, max_prefix_pages]), then their own: q,
+    block_table, ctx_lens, n_shards and max_shards as for ``attn_decode_split``.  Returns (out bf16
+    [B, Hq, D], lse fp32 [B, Hq]), or with ``pair`` (out fp32 [B, 1, Hq, D], lse [B, 1, Hq]), the one
+    slot that ``attn_combine_current`` and ``attn_combine_current_append`` take."""
+    return SharedDecodePlan(q, k_cache, v_cache, prefix_table, prefix_lens, group_rows, block_table,
+                            ctx_lens, n_shards, max_shards, scale, out, lse, workspace, max_pages,
+                            want_lse, pair)()
 
 
 def schedule_simulate(arrival, attn_time, n_layers, wiring="qfirst", ffn_time=1.0, min_batch=2,

@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libqfattn.so")
 SOURCES = ["qfattn_api.hip", "decode_split.hip", "decode_noalloc.hip", "merge.hip", "kv_append.hip",
-           "block_ops.hip", "schedule.cpp"]
+           "block_ops.hip", "rope_append.hip", "rows_attn.hip", "schedule.cpp"]
 ARCH = "gfx950"
 
 # Packed-FP32 instructions are disabled for every HIP translation unit; hipcc's host pass does not

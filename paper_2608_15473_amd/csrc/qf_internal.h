@@ -125,6 +125,72 @@ struct AppendParams {
 };
 
 hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream);
+
+// Norm, rotation and cache append of packed new tokens (rope_append.hip).
+struct RopeAppendParams {
+  const uint16_t* q;            // bf16, token t's heads at q + t * q_stride; null: no queries
+  const uint16_t* k;            // likewise; null (with v): nothing is appended
+  const uint16_t* v;
+  int64_t q_stride, k_stride, v_stride;
+  const uint16_t* q_gain;       // bf16 [D] or null (no norm)
+  const uint16_t* k_gain;
+  const double* freqs;          // fp64 [rotary / 2], radians per position
+  uint16_t* q_out;              // bf16 [tokens, Hq, D]; may be q itself
+  uint16_t* k_cache;            // bf16 [num_pages, Hkv, P, D]
+  uint16_t* v_cache;
+  const int32_t* block_table;   // [B, max_pages] or null (identity)
+  const int32_t* ctx_lens;      // [B]
+  const int32_t* cu_tokens;     // [B + 1] or null (one token per request)
+  int32_t* status;              // optional: set to 1 when a token's append is skipped
+  int32_t batch, tokens, hq, hkv, max_pages, num_pages, rotary;
+  bool interleaved;
+  float eps, amplitude;
+};
+hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t stream);
+
+// Attention of packed query rows over a paged cache (rows_attn.hip): sequence b's rows cu[b] ..
+// cu[b + 1] - 1 see its first ctx_lens[b] positions, and with `causal` row i also positions up to
+// ctx_lens[b] + i.
+struct RowsParams {
+  const uint16_t* q;            // bf16 [rows, Hq, D]
+  const uint16_t* k;            // bf16 [num_pages, Hkv, P, D]
+  const uint16_t* v;
+  const int32_t* block_table;   // [seqs, max_pages] or null (identity)
+  const int32_t* ctx_lens;      // [seqs]
+  const int32_t* cu;            // [seqs + 1]
+  uint16_t* out;                // bf16 [rows, Hq, D], with part_o null
+  float* lse;                   // fp32 [rows, Hq] or null
+  float* part_o;                // fp32 [rows, splits, Hq, D] or null
+  float* part_lse;              // fp32 [rows, splits, Hq]
+  int32_t seqs, rows, hq, hkv, max_pages, num_pages;
+  int32_t tiles;                // bound on the row tiles of one KV head (rows_tiles)
+  int32_t splits;               // ranges that a tile's keys are cut into
+  bool causal;
+  float scale_log2;             // softmax scale * log2(e)
+};
+constexpr int kRowsTile = 128;  // query rows (tokens x query heads of a KV head) of a workgroup
+constexpr int kKeyTile = 64;    // positions of a step
+// Every sequence has at most one tile that is not full.
+inline int64_t rows_tiles(int64_t rows, int64_t group, int64_t seqs) {
+  return rows * group / kRowsTile + (seqs < rows ? seqs : rows);
+}
+hipError_t launch_rows_attn(const RowsParams& p, hipStream_t stream);
+
+// The pairs of one or two sources joined per (row, head): rows of no sequence of `cu` have no pairs in
+// the first source, and are not written where there is no second.
+struct JoinParams {
+  const float* a_o;             // fp32 [rows, a_entries, Hq, D]
+  const float* a_lse;
+  const float* b_o;             // fp32 [rows, b_entries, Hq, D]
+  const float* b_lse;
+  const int32_t* cu;            // [seqs + 1]
+  void* out;                    // bf16 [rows, Hq, D], or fp32 with `pair`
+  float* lse;                   // fp32 [rows, Hq] or null
+  int32_t seqs, rows, hq, a_entries, b_entries;   // b_entries == 0: no second source
+  bool pair;
+};
+hipError_t launch_join(const JoinParams& p, hipStream_t stream);
+
 // out = W . P(x) (+ residual) for a few input rows (block_ops.hip).
 constexpr int kProNone = 0, kProRmsNorm = 1, kProSwiglu = 2;
 constexpr int kLinearMaxRows = 8;

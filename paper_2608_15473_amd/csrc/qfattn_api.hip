@@ -280,6 +280,80 @@ int finish_split(const Split& sp, hipStream_t s) {
   return QF_OK;
 }
 
+// Workgroups of one launch: a grid's work items are counted in 32 bits, at 256 a workgroup.
+constexpr int64_t kMaxGrid = (1 << 24) - 1;
+
+// Ranges that every row tile's keys are cut into: one, or, where there are fewer tiles than the chip keeps
+// resident (two workgroups a compute unit), as many as fill it, each of kMinKeySteps steps at least at the
+// table's capacity.  They depend on the shape alone, so a shape always has the same sums.
+constexpr int64_t kRowsResident = 512;
+constexpr int64_t kMinKeySteps = 4;
+int64_t rows_splits(int64_t tiles, int64_t hkv, int64_t max_pages) {
+  const int64_t steps = (max_pages * qf::kPage + qf::kKeyTile - 1) / qf::kKeyTile;
+  return std::max<int64_t>(1, std::min(kRowsResident / std::max<int64_t>(1, tiles * hkv),
+                                       steps / kMinKeySteps));
+}
+
+// The floats of pairs [rows, entries, Hq, D + 1], the vectors first, rounded up to 16 bytes.
+size_t pair_floats(int64_t rows, int64_t entries, int64_t hq) {
+  return ((size_t)rows * entries * hq * (qf::kHeadDim + 1) + 3) / 4 * 4;
+}
+
+struct Prefill {
+  int64_t tiles, splits;
+  size_t bytes;
+};
+int plan_prefill(const qf_decode_desc* desc, int32_t n_tokens, Prefill* pl) {
+  const int rc = check_desc(desc);
+  if (rc) return rc;
+  if (n_tokens < 0) return fail(QF_EINVAL, "n_tokens %d < 0", n_tokens);
+  const int64_t group = desc->n_q_heads / desc->n_kv_heads;
+  if ((int64_t)n_tokens * group > INT32_MAX - qf::kRowsTile)
+    return fail(QF_EINVAL, "n_tokens %d too large", n_tokens);
+  if (desc->batch == 0 || n_tokens == 0) {
+    *pl = Prefill{0, 1, 0};
+    return QF_OK;
+  }
+  pl->tiles = qf::rows_tiles(n_tokens, group, desc->batch);
+  pl->splits = rows_splits(pl->tiles, desc->n_kv_heads, desc->max_pages_per_seq);
+  pl->bytes = pl->splits > 1
+                  ? pair_floats(n_tokens, pl->splits, desc->n_q_heads) * sizeof(float) : 0;
+  // The most workgroups of a launch, and the rows of the join.
+  if (pl->tiles * pl->splits * desc->n_kv_heads > kMaxGrid ||
+      (pl->splits > 1 && (int64_t)n_tokens * desc->n_q_heads > kMaxGrid))
+    return fail(QF_EINVAL, "too many row tiles for one launch (%d tokens)", n_tokens);
+  return QF_OK;
+}
+
+struct Shared {
+  int64_t tiles, splits, slots;       // slots: shards x chunks of the requests' own positions
+  size_t prefix_floats, bytes;
+};
+int plan_shared(const qf_decode_desc* desc, int32_t n_groups, int32_t max_prefix_pages, Shared* pl) {
+  const int rc = check_desc(desc);
+  if (rc) return rc;
+  const qf_decode_desc& d = *desc;
+  if (n_groups < 0) return fail(QF_EINVAL, "n_groups %d < 0", n_groups);
+  if (n_groups > 0 && (max_prefix_pages < 1 || (int64_t)max_prefix_pages * qf::kPage > INT32_MAX))
+    return fail(QF_EINVAL, "max_prefix_pages %d out of range", max_prefix_pages);
+  const int64_t group = d.n_q_heads / d.n_kv_heads;
+  if ((int64_t)d.batch * d.n_q_heads > kMaxGrid)
+    return fail(QF_EINVAL, "batch * n_q_heads too large");
+  *pl = Shared{0, 1, 0, 0, 0};
+  if (d.batch == 0) return QF_OK;
+  pl->slots = d.max_shards * choose_chunks(&d);
+  if (pl->slots > INT32_MAX) return fail(QF_EINVAL, "max_shards * chunks exceeds int32");
+  if (n_groups > 0) {
+    pl->tiles = qf::rows_tiles(d.batch, group, n_groups);
+    pl->splits = rows_splits(pl->tiles, d.n_kv_heads, max_prefix_pages);
+    pl->prefix_floats = pair_floats(d.batch, pl->splits, d.n_q_heads);
+    if (pl->tiles * pl->splits * d.n_kv_heads > kMaxGrid)
+      return fail(QF_EINVAL, "too many row tiles for one launch (%d requests)", d.batch);
+  }
+  pl->bytes = (pl->prefix_floats + pair_floats(d.batch, pl->slots, d.n_q_heads)) * sizeof(float);
+  return QF_OK;
+}
+
 // Everything qf_linear checks and derives before launching.
 int prepare_linear(const qf_linear_args* a, qf::LinearParams* out_p, bool* noop) {
   const int32_t rows = a->rows, n_out = a->n_out, k = a->k;
@@ -840,6 +914,242 @@ int qf_attn_decode_split_beside(const qf_decode_desc* desc, const void* q, const
     e = qf::launch_decode_split_beside(sp.p, sp.group, lp, s);
   if (e != hipSuccess) return fail(QF_EHIP, "decode_split_beside launch: %s", hipGetErrorString(e));
   return sp.noop ? QF_OK : finish_split(sp, s);
+}
+
+int qf_qkv_rope_append(const qf_decode_desc* desc, int32_t n_tokens, const int32_t* cu_tokens,
+                       const int32_t* ctx_lens, const qf_rope* rope, const void* q, int64_t q_stride,
+                       const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                       const void* q_gain, const void* k_gain, float eps, void* q_out, void* k_cache,
+                       void* v_cache, const int32_t* block_table, int32_t* status, void* stream) {
+  g_error[0] = 0;
+  const int rc = check_desc(desc);
+  if (rc) return rc;
+  const qf_decode_desc& d = *desc;
+  if (n_tokens < 0) return fail(QF_EINVAL, "n_tokens %d < 0", n_tokens);
+  if (n_tokens > kMaxGrid) return fail(QF_EINVAL, "n_tokens %d too large", n_tokens);
+  if (!cu_tokens && n_tokens != d.batch)
+    return fail(QF_EINVAL, "without cu_tokens there is one token per request (%d tokens, batch %d)",
+                n_tokens, d.batch);
+  if (rope) {
+    if (rope->layout != QF_ROPE_HALF && rope->layout != QF_ROPE_INTERLEAVED)
+      return fail(QF_EINVAL, "unknown rope layout %d", rope->layout);
+    if (rope->rotary_dim < 0 || rope->rotary_dim > qf::kHeadDim)
+      return fail(QF_EINVAL, "rotary_dim %d not in [0, %d]", rope->rotary_dim, qf::kHeadDim);
+    if (rope->rotary_dim % 16)
+      return fail(QF_EUNSUPPORTED, "rotary_dim %d is not a multiple of 16", rope->rotary_dim);
+    if (!isfinite(rope->amplitude)) return fail(QF_EINVAL, "rope amplitude is not finite");
+  }
+  if ((q_gain || k_gain) && !(eps >= 0.0f)) return fail(QF_EINVAL, "eps must be >= 0");
+  if (!k != !v) return fail(QF_EINVAL, "k and v go together");
+  if (!q && !k) return fail(QF_EINVAL, "neither queries nor keys are given");
+  if ((q && (q_stride < (int64_t)d.n_q_heads * qf::kHeadDim || q_stride % 8)) ||
+      (k && (k_stride < (int64_t)d.n_kv_heads * qf::kHeadDim || k_stride % 8 ||
+             v_stride < (int64_t)d.n_kv_heads * qf::kHeadDim || v_stride % 8)))
+    return fail(QF_EINVAL, "strides must be multiples of 8 and at least a row's heads");
+  if (d.batch == 0 || n_tokens == 0) return QF_OK;
+  if (!ctx_lens || (q && !q_out) || (k && (!k_cache || !v_cache)) ||
+      (rope && rope->rotary_dim > 0 && !rope->freqs))
+    return fail(QF_EINVAL, "a required pointer is NULL");
+  if (q_out == q && q && q_stride != (int64_t)d.n_q_heads * qf::kHeadDim)
+    return fail(QF_EINVAL, "queries are rotated in place only where their rows are contiguous");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_gain, 16) ||
+      !aligned(k_gain, 16) || !aligned(q_out, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return fail(QF_EALIGN, "q, k, v, the gains, q_out and the caches must be 16-byte aligned");
+  if (!aligned(cu_tokens, 4) || !aligned(ctx_lens, 4) || !aligned(block_table, 4) ||
+      !aligned(status, 4) || (rope && !aligned(rope->freqs, 8)))
+    return fail(QF_EALIGN, "index arrays and status must be 4-byte aligned, freqs 8-byte");
+  if (k && !block_table && (int64_t)d.batch * d.max_pages_per_seq > d.num_pages)
+    return fail(QF_EINVAL, "identity block table needs num_pages >= batch * max_pages_per_seq");
+  qf::RopeAppendParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.q_gain = static_cast<const uint16_t*>(q_gain);
+  p.k_gain = static_cast<const uint16_t*>(k_gain);
+  p.freqs = rope ? rope->freqs : nullptr;
+  p.q_out = static_cast<uint16_t*>(q_out);
+  p.k_cache = static_cast<uint16_t*>(k_cache);
+  p.v_cache = static_cast<uint16_t*>(v_cache);
+  p.block_table = block_table;
+  p.ctx_lens = ctx_lens;
+  p.cu_tokens = cu_tokens;
+  p.status = status;
+  p.batch = d.batch;
+  p.tokens = n_tokens;
+  p.hq = d.n_q_heads;
+  p.hkv = d.n_kv_heads;
+  p.max_pages = d.max_pages_per_seq;
+  p.num_pages = d.num_pages;
+  p.rotary = rope ? rope->rotary_dim : 0;
+  p.interleaved = rope && rope->layout == QF_ROPE_INTERLEAVED;
+  p.eps = eps;
+  p.amplitude = rope ? rope->amplitude : 1.0f;
+  const hipError_t e = qf::launch_rope_append(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(QF_EHIP, "rope_append launch: %s", hipGetErrorString(e));
+  return QF_OK;
+}
+
+int qf_attn_prefill_workspace_size(const qf_decode_desc* desc, int32_t n_tokens, size_t* bytes) {
+  g_error[0] = 0;
+  Prefill pl;
+  const int rc = plan_prefill(desc, n_tokens, &pl);
+  if (rc) return rc;
+  if (!bytes) return fail(QF_EINVAL, "bytes is NULL");
+  *bytes = pl.bytes;
+  return QF_OK;
+}
+
+int qf_attn_prefill(const qf_decode_desc* desc, int32_t n_tokens, const void* q, const void* k_cache,
+                    const void* v_cache, const int32_t* block_table, const int32_t* ctx_lens,
+                    const int32_t* cu_tokens, void* out, float* lse, void* workspace,
+                    size_t workspace_size, void* stream) {
+  g_error[0] = 0;
+  Prefill pl;
+  const int rc = plan_prefill(desc, n_tokens, &pl);
+  if (rc) return rc;
+  const qf_decode_desc& d = *desc;
+  if (d.batch == 0 || n_tokens == 0) return QF_OK;
+  if (!q || !k_cache || !v_cache || !ctx_lens || !cu_tokens || !out)
+    return fail(QF_EINVAL, "a required pointer is NULL");
+  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 8))
+    return fail(QF_EALIGN, "q, k_cache and v_cache must be 16-byte aligned, out 8-byte");
+  if (!aligned(lse, 4) || !aligned(ctx_lens, 4) || !aligned(cu_tokens, 4) || !aligned(block_table, 4))
+    return fail(QF_EALIGN, "lse, ctx_lens, cu_tokens and block_table must be 4-byte aligned");
+  if (!block_table && (int64_t)d.batch * d.max_pages_per_seq > d.num_pages)
+    return fail(QF_EINVAL, "identity block table needs num_pages >= batch * max_pages_per_seq");
+  if (pl.bytes) {
+    if (!workspace) return fail(QF_EINVAL, "this shape needs %zu bytes of workspace", pl.bytes);
+    if (workspace_size < pl.bytes)
+      return fail(QF_EINVAL, "workspace of %zu bytes < %zu needed", workspace_size, pl.bytes);
+    if (!aligned(workspace, 16)) return fail(QF_EALIGN, "workspace must be 16-byte aligned");
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  qf::RowsParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k_cache);
+  p.v = static_cast<const uint16_t*>(v_cache);
+  p.block_table = block_table;
+  p.ctx_lens = ctx_lens;
+  p.cu = cu_tokens;
+  p.seqs = d.batch;
+  p.rows = n_tokens;
+  p.hq = d.n_q_heads;
+  p.hkv = d.n_kv_heads;
+  p.max_pages = d.max_pages_per_seq;
+  p.num_pages = d.num_pages;
+  p.tiles = (int32_t)pl.tiles;
+  p.splits = (int32_t)pl.splits;
+  p.causal = true;
+  p.scale_log2 = (float)((double)d.softmax_scale * 1.4426950408889634);
+  if (pl.splits > 1) {
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = p.part_o + (size_t)n_tokens * pl.splits * d.n_q_heads * qf::kHeadDim;
+  } else {
+    p.out = static_cast<uint16_t*>(out);
+    p.lse = lse;
+  }
+  hipError_t e = qf::launch_rows_attn(p, s);
+  if (e != hipSuccess) return fail(QF_EHIP, "prefill launch: %s", hipGetErrorString(e));
+  if (pl.splits == 1) return QF_OK;
+  qf::JoinParams j{};
+  j.a_o = p.part_o;
+  j.a_lse = p.part_lse;
+  j.cu = cu_tokens;
+  j.out = out;
+  j.lse = lse;
+  j.seqs = d.batch;
+  j.rows = n_tokens;
+  j.hq = d.n_q_heads;
+  j.a_entries = p.splits;
+  e = qf::launch_join(j, s);
+  if (e != hipSuccess) return fail(QF_EHIP, "prefill join launch: %s", hipGetErrorString(e));
+  return QF_OK;
+}
+
+int qf_attn_decode_shared_workspace_size(const qf_decode_desc* desc, int32_t n_groups,
+                                         int32_t max_prefix_pages, size_t* bytes) {
+  g_error[0] = 0;
+  Shared pl;
+  const int rc = plan_shared(desc, n_groups, max_prefix_pages, &pl);
+  if (rc) return rc;
+  if (!bytes) return fail(QF_EINVAL, "bytes is NULL");
+  *bytes = pl.bytes;
+  return QF_OK;
+}
+
+int qf_attn_decode_shared(const qf_decode_desc* desc, const void* q, const void* k_cache,
+                          const void* v_cache, int32_t n_groups, int32_t max_prefix_pages,
+                          const int32_t* prefix_table, const int32_t* prefix_lens,
+                          const int32_t* group_rows, const int32_t* block_table,
+                          const int32_t* ctx_lens, const int32_t* n_shards, int32_t pair, void* out,
+                          float* lse, void* workspace, size_t workspace_size, void* stream) {
+  g_error[0] = 0;
+  Shared pl;
+  int rc = plan_shared(desc, n_groups, max_prefix_pages, &pl);
+  if (rc) return rc;
+  const qf_decode_desc& d = *desc;
+  if (d.batch == 0) return QF_OK;
+  if (!out || (pair && !lse) || !workspace ||
+      (n_groups > 0 && (!prefix_table || !prefix_lens || !group_rows)))
+    return fail(QF_EINVAL, "a required pointer is NULL");
+  if (!aligned(out, pair ? 16 : 4) || !aligned(lse, 4) || !aligned(workspace, 16) ||
+      !aligned(prefix_table, 4) || !aligned(prefix_lens, 4) || !aligned(group_rows, 4))
+    return fail(QF_EALIGN, "workspace and a pair's out must be 16-byte aligned, the others 4-byte");
+  if (workspace_size < pl.bytes)
+    return fail(QF_EINVAL, "workspace of %zu bytes < %zu needed", workspace_size, pl.bytes);
+  float* const prefix_o = static_cast<float*>(workspace);
+  float* const own_o = prefix_o + pl.prefix_floats;
+  float* const own_lse = own_o + (size_t)d.batch * pl.slots * d.n_q_heads * qf::kHeadDim;
+  Split sp;
+  rc = prepare_split(desc, q, k_cache, v_cache, block_table, ctx_lens, n_shards, own_o, own_lse,
+                     nullptr, 0, &sp, false, false);
+  if (rc || sp.noop) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  qf::JoinParams j{};
+  if (n_groups > 0) {
+    qf::RowsParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(k_cache);
+    p.v = static_cast<const uint16_t*>(v_cache);
+    p.block_table = prefix_table;
+    p.ctx_lens = prefix_lens;
+    p.cu = group_rows;
+    p.part_o = prefix_o;
+    p.part_lse = prefix_o + (size_t)d.batch * pl.splits * d.n_q_heads * qf::kHeadDim;
+    p.seqs = n_groups;
+    p.rows = d.batch;
+    p.hq = d.n_q_heads;
+    p.hkv = d.n_kv_heads;
+    p.max_pages = max_prefix_pages;
+    p.num_pages = d.num_pages;
+    p.tiles = (int32_t)pl.tiles;
+    p.splits = (int32_t)pl.splits;
+    p.causal = false;
+    p.scale_log2 = (float)((double)d.softmax_scale * 1.4426950408889634);
+    const hipError_t e = qf::launch_rows_attn(p, s);
+    if (e != hipSuccess) return fail(QF_EHIP, "prefix launch: %s", hipGetErrorString(e));
+    j.a_o = p.part_o;
+    j.a_lse = p.part_lse;
+    j.a_entries = p.splits;
+  }
+  hipError_t e = qf::launch_decode_split(sp.p, sp.group, s);
+  if (e != hipSuccess) return fail(QF_EHIP, "decode_split launch: %s", hipGetErrorString(e));
+  j.b_o = own_o;
+  j.b_lse = own_lse;
+  j.b_entries = (int32_t)pl.slots;
+  j.cu = group_rows;
+  j.out = out;
+  j.lse = lse;
+  j.seqs = n_groups;
+  j.rows = d.batch;
+  j.hq = d.n_q_heads;
+  j.pair = pair != 0;
+  e = qf::launch_join(j, s);
+  if (e != hipSuccess) return fail(QF_EHIP, "join launch: %s", hipGetErrorString(e));
+  return QF_OK;
 }
 
 int qf_schedule_simulate(int32_t n_requests, const double* arrival, const double* attn_time,
