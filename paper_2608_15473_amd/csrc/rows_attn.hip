@@ -19,6 +19,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "merge_body.h"
 #include "qf_internal.h"
 #include "row_owner.h"
@@ -53,6 +55,35 @@ __device__ __forceinline__ int slot(int i, int ch) { return ch ^ (4 * (i & 3) + 
 __device__ __forceinline__ float other_half(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// One page of K and one of V (4 KB each) from global memory straight to LDS, by one wavefront: load j takes
+// rows 4 j .. 4 j + 3, lane l from page + 1024 j + at[j] to LDS byte to + 1024 j + 16 l.  Written as one
+// block because the compiler, which cannot tell the two LDS buffers apart, would wait for the loads before
+// every transposed read of the other buffer; whoever reads the page waits by hand (arrived()).  No output
+// registers; M0 holds the LDS base, which the loads may follow after one wait state (the compiler reserves
+// M0 and sets it before each use of its own).
+__device__ __forceinline__ void load_page(const void* k, const void* v, const int (&at)[4], uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %6\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %0\n\t"
+      "global_load_lds_dwordx4 %3, %0 offset:1024\n\t"
+      "global_load_lds_dwordx4 %4, %0 offset:2048\n\t"
+      "global_load_lds_dwordx4 %5, %0 offset:3072\n\t"
+      "s_mov_b32 m0, %7\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %1\n\t"
+      "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+      "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
+      "global_load_lds_dwordx4 %5, %1 offset:3072"
+      :
+      : "s"(k), "s"(v), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(to), "s"(to + kTileBytes)
+      : "memory");
+}
+// Every load of this wavefront has arrived; then every wavefront's.
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // The sequence and first row of a workgroup's tile; every wavefront computes it for itself.
@@ -103,7 +134,7 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
 }
 
 __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char s_k[kTileBytes], s_v[kTileBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[4 * kTileBytes];   // 2 x (K, V)
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
@@ -174,43 +205,55 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
 
   // Lane addresses.  Scores: key 32 t + (lane & 31), chunk 2 kk + half.  V: lane group of 16 reads 4 keys
   // by 16 dims, key 8 r + 4 half + (lane & 15) / 4 of the step's 16, dims 32 d + 16 ((lane >> 4) & 1) + ...
-  const int krow = lane & 15;
-  const int kbase = (lane & 31) * (D * 2);
-  const int vi = (lane & 15) >> 2;
-  const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  // Both are a lane's base with the chunk's higher bits exclusive-or'ed in (slot()).
+  const int kbase = (lane & 31) * (D * 2) + slot(lane & 15, half) * 16;
+  const int vrow = 4 * half + ((lane & 15) >> 2);
+  const int vbase = kTileBytes + vrow * (D * 2) +
+                    slot(vrow, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
 
-  for (int kt = k0; kt < k1; ++kt) {
-    // Stage the step's 4 pages, one per wavefront.  The page past the last repeats it (its keys are
-    // masked); one outside the pool is read as page 0 and its scores become NaN.
-    int bad = 0;
-    int64_t mine = 0;
+  // A step's 4 pages go straight to LDS, one per wavefront.  The lanes' places there are consecutive, so
+  // the swizzle is in the addresses that they read from.  A page past the last repeats it (its keys are
+  // masked); one outside the pool is read as page 0 and its scores become NaN.
+  int at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    at[j] = (lane >> 4) * (D * 2) + ((lane & 15) ^ (4 * (lane >> 4) + j)) * 16;
+  struct Pages {
+    int of[kPagesPerTile];
+  };
+  auto entries = [&](int kt) {           // of step kt, or of the last one
+    Pages e;
+#pragma unroll
+    for (int j = 0; j < kPagesPerTile; ++j) e.of[j] = min(kt * kPagesPerTile + j, pages - 1);
+    if (bt) {
+#pragma unroll
+      for (int j = 0; j < kPagesPerTile; ++j) e.of[j] = bt[e.of[j]];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPagesPerTile; ++j) e.of[j] += b * p.max_pages;
+    }
+    return e;
+  };
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)s_kv +
+                       wave * (P * D * 2);
+  // Returns which pages of the step are outside the pool (bit j: page j).
+  auto stage = [&](const Pages& e, int buffer) {
+    int bad = 0, mine = 0;
 #pragma unroll
     for (int j = 0; j < kPagesPerTile; ++j) {
-      const int pg = min(kt * kPagesPerTile + j, pages - 1);
-      int ph = bt ? bt[pg] : b * p.max_pages + pg;
-      if ((unsigned)ph >= (unsigned)p.num_pages) {
-        bad |= 1 << j;
-        ph = 0;
-      }
-      if (j == wave) mine = ph;
+      const bool in = (unsigned)e.of[j] < (unsigned)p.num_pages;
+      bad |= in ? 0 : 1 << j;
+      if (j == wave) mine = in ? e.of[j] : 0;
     }
     const int64_t off = mine * page_stride + head_off;
-    u32x4 kw[4], vw[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      kw[j] = reinterpret_cast<const u32x4*>(p.k + off)[64 * j + lane];
-      vw[j] = reinterpret_cast<const u32x4*>(p.v + off)[64 * j + lane];
-    }
-    __syncthreads();                    // the last step's reads are done
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = 4 * j + (lane >> 4);
-      const int at = wave * (P * D * 2) + i * (D * 2) + slot(i, lane & 15) * 16;
-      *reinterpret_cast<u32x4*>(s_k + at) = kw[j];
-      *reinterpret_cast<u32x4*>(s_v + at) = vw[j];
-    }
-    __syncthreads();
+    load_page(p.k + off, p.v + off, at, lds + buffer * 2 * kTileBytes);
+    return bad;
+  };
 
+  // One step on the keys in `kv`.  MASKED: some row of the wavefront does not see all of them, or a page is
+  // outside the pool.
+  auto step = [&](auto masked, int kt, const unsigned char* kv, int bad) {
+    constexpr bool MASKED = decltype(masked)::value;
     // S^T of 2 x 32 keys.
     f32x16 s[2];
 #pragma unroll
@@ -219,25 +262,18 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
       for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(
-            s_k + t * 32 * D * 2 + kbase + slot(krow, 2 * kk + half) * 16);
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kv + t * 32 * D * 2 + (kbase ^ (32 * kk)));
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[kk], s[t], 0, 0, 0);
       }
     }
-    const bool masked = (kt + 1) * kKeyTile > all_see;   // wavefront-uniform
-    if (bad != 0) {
+    if constexpr (MASKED) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 16; ++i) {
           if ((bad >> (2 * t + i / 8)) & 1) s[t][i] = NAN;
-    }
-    if (masked) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
           if (kt * kKeyTile + 32 * t + 8 * (i / 4) + 4 * half + i % 4 >= sees) s[t][i] = -INFINITY;
+        }
     }
     float top = s[0][0];
 #pragma unroll
@@ -281,13 +317,11 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
         uint2 a[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int i = 8 * r + 4 * half + vi;
-          const unsigned char* at =
-              s_v + (16 * u + i) * (D * 2) + slot(i, 4 * d + vch) * 16 + 8 * (lane & 1);
+          const unsigned char* from = kv + (16 * u + 8 * r) * (D * 2) + (vbase ^ (64 * d + 32 * r));
           a[r] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)at));
+              (__attribute__((address_space(3))) s16x4*)from));
         }
-        if (masked) {                    // a masked key's weight is 0, but 0 times infinity is not
+        if constexpr (MASKED) {          // a masked key's weight is 0, but 0 times infinity is not
           unclean = unclean || bad_pair(a[0].x) || bad_pair(a[0].y) || bad_pair(a[1].x) || bad_pair(a[1].y);
           a[0] = make_uint2(finite_pair(a[0].x), finite_pair(a[0].y));
           a[1] = make_uint2(finite_pair(a[1].x), finite_pair(a[1].y));
@@ -297,7 +331,9 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
                                                        0, 0, 0);
       }
     }
-    if (__any(unclean)) {                // rare: infinities and NaN of the keys that a row does see
+    if constexpr (MASKED) {
+      if (!__any(unclean)) return;
+      // Rare: the infinities and NaN of the keys that a row does see.
 #pragma unroll 1
       for (int key = 0; key < kKeyTile; ++key) {
         const int i = key & 15;
@@ -308,10 +344,36 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
           for (int e = 0; e < 16; ++e) {
             const int dim = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
             const uint32_t x = *reinterpret_cast<const uint16_t*>(
-                s_v + key * (D * 2) + slot(i, dim / 8) * 16 + (dim % 8) * 2);
+                kv + kTileBytes + key * (D * 2) + slot(i, dim / 8) * 16 + (dim % 8) * 2);
             if (seen && (x & 0x7f80u) == 0x7f80u) o[d][e] += mrg::bf16_lo(x);
           }
       }
+    }
+  };
+
+  if (k0 < k1) {
+    int bad = stage(entries(k0), 0), bad_now = 0, kt = k0;
+    Pages next = entries(k0 + 1);
+    // Waits for step kt and requests the next one; returns the keys.
+    auto advance = [&]() -> const unsigned char* {
+      const int buffer = (kt - k0) & 1;
+      bad_now = bad;
+      arrived();                         // the step's keys are here, and the last step's reads are done
+      if (kt + 1 < k1) {
+        bad = stage(next, 1 - buffer);
+        next = entries(kt + 2);
+      }
+      return s_kv + buffer * 2 * kTileBytes;
+    };
+    while (kt < k1) {
+      for (; kt < k1 && (kt + 1) * kKeyTile <= all_see && bad == 0; ++kt) {
+        const unsigned char* const kv = advance();
+        step(std::false_type{}, kt, kv, 0);
+      }
+      if (kt == k1) break;
+      const unsigned char* const kv = advance();
+      step(std::true_type{}, kt, kv, bad_now);
+      ++kt;
     }
   }
 
