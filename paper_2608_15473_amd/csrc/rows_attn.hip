@@ -1,11 +1,11 @@
 // Attention of packed query rows over a paged grouped-query KV cache, on the matrix cores, and the join
 // of the pairs that its key ranges leave.
 //
-// One pass over the keys with a running maximum m of s = q . k and a sum l per row, c = scale * log2 e:
-//   p = exp2(c s - c m),  l = sum p,  o = sum p v,  out = o / l,  lse = (c m + log2 l) ln 2;
-// when c s exceeds c m by more than kLazy, m is raised and l, o scaled by exp2(c m_old - c m_new).  One
-// fused multiply-add makes c s - (c m rounded); all p of a row share the rounding's factor, so it cancels,
-// but past |c m| = kFar it could overflow, and p is exp2(c (s - m)) from then on.
+// One pass over the keys: with s = q . k, c = scale * log2 e and a running reference r per row,
+//   p = exp2(c s - r),  l = sum p,  o = sum p v,  out = o / l,  lse = (r + log2 l) ln 2.
+// Where a score exceeds r by more than kLazy, r is raised to the next whole number above it, and what has
+// been summed is scaled by the power of two between (exact, in the bf16 weights too).  Past |r| = kFar
+// whole numbers are as coarse as fp32 scores: such rows keep the maximum m itself, p = exp2(c (s - m)).
 //
 // A workgroup takes one KV head and a tile of 128 query rows, a row being (token, query head of the
 // group), so that the G query heads of a KV head share every key read.  Its 4 wavefronts have 32 rows
@@ -28,6 +28,7 @@
 namespace qf {
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -39,9 +40,13 @@ constexpr int W = 4;                     // wavefronts of a workgroup
 constexpr int kRowsPerWave = kRowsTile / W;
 constexpr int kPagesPerTile = kKeyTile / P;
 constexpr int kTileBytes = kKeyTile * D * 2;
+constexpr int kBufferBytes = 2 * kTileBytes;         // K and V of a step
+constexpr int kUnit = kKeyTile / 2;                  // keys that the pipeline takes at a time
+constexpr int kUnitBytes = kUnit * D * 2;
+constexpr int kRing = 4;                             // fragments in registers
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;            // log2 units: p <= 256 between rescales
-constexpr float kFar = 1048576.0f;       // log2 units: up to here c m is rounded by 2^-4 at most
+constexpr float kFar = 1048576.0f;       // log2 units
 static_assert(kPagesPerTile == W, "a wavefront stages one page of each step");
 
 typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
@@ -57,28 +62,22 @@ __device__ __forceinline__ float other_half(float x) {
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// One page of K and one of V (4 KB each) from global memory straight to LDS, by one wavefront: load j takes
-// rows 4 j .. 4 j + 3, lane l from page + 1024 j + at[j] to LDS byte to + 1024 j + 16 l.  Written as one
-// block because the compiler, which cannot tell the two LDS buffers apart, would wait for the loads before
-// every transposed read of the other buffer; whoever reads the page waits by hand (arrived()).  No output
-// registers; M0 holds the LDS base, which the loads may follow after one wait state (the compiler reserves
-// M0 and sets it before each use of its own).
-__device__ __forceinline__ void load_page(const void* k, const void* v, const int (&at)[4], uint32_t to) {
+// One page (4 KB) from global memory straight to LDS, by one wavefront: load j takes rows 4 j .. 4 j + 3,
+// lane l from page + 1024 j + (at ^ 16 j) to LDS byte to + 1024 j + 16 l.  Written as one block because the
+// compiler, which cannot tell the LDS buffers apart, would wait for the loads before every transposed read
+// of another buffer; whoever reads the page waits by hand (arrived()).  No output registers; M0 holds the
+// LDS base, which the loads may follow after one wait state (the compiler reserves M0 and sets it before
+// each use of its own).
+__device__ __forceinline__ void load_page(const void* page, int at, uint32_t to) {
   asm volatile(
-      "s_mov_b32 m0, %6\n\t"
+      "s_mov_b32 m0, %5\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %0\n\t"
-      "global_load_lds_dwordx4 %3, %0 offset:1024\n\t"
-      "global_load_lds_dwordx4 %4, %0 offset:2048\n\t"
-      "global_load_lds_dwordx4 %5, %0 offset:3072\n\t"
-      "s_mov_b32 m0, %7\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %1\n\t"
-      "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-      "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
-      "global_load_lds_dwordx4 %5, %1 offset:3072"
+      "global_load_lds_dwordx4 %1, %0\n\t"
+      "global_load_lds_dwordx4 %2, %0 offset:1024\n\t"
+      "global_load_lds_dwordx4 %3, %0 offset:2048\n\t"
+      "global_load_lds_dwordx4 %4, %0 offset:3072"
       :
-      : "s"(k), "s"(v), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(to), "s"(to + kTileBytes)
+      : "s"(page), "v"(at), "v"(at ^ 16), "v"(at ^ 32), "v"(at ^ 48), "s"(to)
       : "memory");
 }
 // Every load of this wavefront has arrived; then every wavefront's.
@@ -124,9 +123,7 @@ __device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ cu, int32_
   return Tile{-1, 0, 0, 0};
 }
 
-__device__ __forceinline__ bool bad_pair(uint32_t w) {   // a bf16 of the pair is infinite or NaN
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
+// A bf16 pair with zeros for infinities and NaN.
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
   if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
@@ -134,7 +131,8 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
 }
 
 __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[4 * kTileBytes];   // 2 x (K, V)
+  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2 * kBufferBytes];
+  __shared__ int s_found;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
@@ -193,9 +191,9 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  // m starts at the lowest finite value, and so does cm = c m: no difference is inf - inf.
-  float m = -FLT_MAX, cm = -FLT_MAX, l = 0.0f;
-  bool far = false;                      // wavefront-uniform: some row is past kFar
+  // The reference starts at the lowest finite value: no difference is inf - inf.
+  float m = -FLT_MAX, less = -FLT_MAX, l = 0.0f;   // less: the reference, 0 where m is it
+  bool is_far = false, far = false;      // m is, for this row, for some row of the wavefront
 
   const int pages = (keys + P - 1) / P;
   const const_i32_ptr bt =
@@ -206,18 +204,27 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
   // Lane addresses.  Scores: key 32 t + (lane & 31), chunk 2 kk + half.  V: lane group of 16 reads 4 keys
   // by 16 dims, key 8 r + 4 half + (lane & 15) / 4 of the step's 16, dims 32 d + 16 ((lane >> 4) & 1) + ...
   // Both are a lane's base with the chunk's higher bits exclusive-or'ed in (slot()).
-  const int kbase = (lane & 31) * (D * 2) + slot(lane & 15, half) * 16;
-  const int vrow = 4 * half + ((lane & 15) >> 2);
-  const int vbase = kTileBytes + vrow * (D * 2) +
-                    slot(vrow, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+  // They are kept, and toggled between the two buffers once a step.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)s_kv;
+  uint32_t ka[8], va[8];
+  {
+    const int kbase = (lane & 31) * (D * 2) + slot(lane & 15, half) * 16;
+    const int vrow = 4 * half + ((lane & 15) >> 2);
+    const int vbase = vrow * (D * 2) + slot(vrow, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 +
+                      8 * (lane & 1);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) ka[kk] = lds0 + (kbase ^ (32 * kk));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        va[2 * d + r] = lds0 + kTileBytes + 8 * r * (D * 2) + (vbase ^ (64 * d + 32 * r));
+  }
 
   // A step's 4 pages go straight to LDS, one per wavefront.  The lanes' places there are consecutive, so
   // the swizzle is in the addresses that they read from.  A page past the last repeats it (its keys are
   // masked); one outside the pool is read as page 0 and its scores become NaN.
-  int at[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    at[j] = (lane >> 4) * (D * 2) + ((lane & 15) ^ (4 * (lane >> 4) + j)) * 16;
+  const int at = (lane >> 4) * (D * 2) + ((lane & 15) ^ (4 * (lane >> 4))) * 16;
   struct Pages {
     int of[kPagesPerTile];
   };
@@ -234,146 +241,232 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
     }
     return e;
   };
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)s_kv +
-                       wave * (P * D * 2);
-  // Returns which pages of the step are outside the pool (bit j: page j).
-  auto stage = [&](const Pages& e, int buffer) {
-    int bad = 0, mine = 0;
+  const uint32_t lds = lds0 + wave * (P * D * 2);
+  // This wavefront's page of a step; bit j of bad: page j is outside the pool.
+  auto my_page = [&](const Pages& e, int& bad) {
+    int mine = 0;
+    bad = 0;
 #pragma unroll
     for (int j = 0; j < kPagesPerTile; ++j) {
       const bool in = (unsigned)e.of[j] < (unsigned)p.num_pages;
       bad |= in ? 0 : 1 << j;
       if (j == wave) mine = in ? e.of[j] : 0;
     }
-    const int64_t off = mine * page_stride + head_off;
-    load_page(p.k + off, p.v + off, at, lds + buffer * 2 * kTileBytes);
-    return bad;
+    return mine;
+  };
+  auto load_k = [&](int page, int to) { load_page(p.k + page * page_stride + head_off, at, lds + to); };
+  auto load_v = [&](int page, int to) {
+    load_page(p.v + page * page_stride + head_off, at, lds + to + kTileBytes);
   };
 
-  // One step on the keys in `kv`.  MASKED: some row of the wavefront does not see all of them, or a page is
-  // outside the pool.
-  auto step = [&](auto masked, int kt, const unsigned char* kv, int bad) {
-    constexpr bool MASKED = decltype(masked)::value;
-    // S^T of 2 x 32 keys.
-    f32x16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kv + t * 32 * D * 2 + (kbase ^ (32 * kk)));
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[kk], s[t], 0, 0, 0);
+  // From step `edge` on, some row of the tile does not see every key.  A masked key's weight is 0, but 0
+  // times an infinity or NaN is not: so every wavefront makes zeros of those in its page of V.  Where there
+  // were any (rare), they are added at the end to the rows that do see them.
+  const int edge = max(k0, (poison ? 0 : p.causal ? n0 + (tile.first >> gshift) + 1 : n0) / kKeyTile);
+  auto clean = [&](int buffer) {
+    unsigned char* const mine = s_kv + buffer + kTileBytes + wave * (P * D * 2);
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+      uint4* const at4 = reinterpret_cast<uint4*>(mine + 1024 * j) + lane;
+      const uint4 x = *at4;
+      const uint4 y = make_uint4(finite_pair(x.x), finite_pair(x.y), finite_pair(x.z), finite_pair(x.w));
+      if (((x.x ^ y.x) | (x.y ^ y.y) | (x.z ^ y.z) | (x.w ^ y.w)) != 0) {
+        *at4 = y;
+        s_found = 1;
       }
     }
-    if constexpr (MASKED) {
+    __syncthreads();
+  };
+
+  // A fragment of K or V for one matrix instruction: of K (i < 8) the unit's 32 keys by dims 16 i .. + 15, of V
+  // 16 keys by 32 dims.
+  auto fragment = [&](int unit, int i) __attribute__((always_inline)) -> bf16x8 {
+    if (i < 8)
+      return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(ka[i] + unit * kUnitBytes);
+    const int d = i & 3, u = (i - 8) >> 2;
+    s16x4 a[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+    for (int r = 0; r < 2; ++r)
+      a[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(
+          va[2 * d + r] + unit * kUnitBytes + 16 * u * (D * 2)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // The highest of a unit's scores that the row sees.
+  auto highest = [&](const f32x16& n) __attribute__((always_inline)) {
+    float top = n[0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if ((bad >> (2 * t + i / 8)) & 1) s[t][i] = NAN;
-          if (kt * kKeyTile + 32 * t + 8 * (i / 4) + 4 * half + i % 4 >= sees) s[t][i] = -INFINITY;
-        }
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-    top = fmaxf(top, other_half(top));
-    if (__any((top - m) * scale > kLazy)) {
-      const float raised = fmaxf(m, top), c_raised = fmaxf(raised * scale, -FLT_MAX);
-      far = far || __any(fabsf(c_raised) > kFar && raised > -FLT_MAX);
-      const float f = exp2f(far ? (m - raised) * scale : cm - c_raised);
-      m = raised;
-      cm = c_raised;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-    }
-    if (far) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] -= m;
-    }
-    const float less = far ? 0.0f : cm;
-    bf16x8 w[4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, n[i]);
+    return top;
+  };
+  // Scores n, from position key0 on, are next to be weighed, their highest being `top`: where some are masked
+  // or in a bad page they are made so first, and where one is far above the reference, that is raised and
+  // what was summed at the old one, weights w whose product is still to come among it, scaled.
+  auto take = [&](f32x16& n, float top, u32x4 (&w)[2], int key0, int bad) __attribute__((always_inline)) {
+    if (key0 + kUnit > all_see || bad != 0) {
+      asm volatile("");                  // a branch, not 64 selections
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale, -less));
-        l += e;
-        w[2 * t + i / 8][i % 8] = (__bf16)e;
+        if ((bad >> (i / 8)) & 1) n[i] = NAN;
+        if (key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) n[i] = -INFINITY;
       }
-
-    // O^T += V^T P^T.
-    bool unclean = false;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        uint2 a[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const unsigned char* from = kv + (16 * u + 8 * r) * (D * 2) + (vbase ^ (64 * d + 32 * r));
-          a[r] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)from));
-        }
-        if constexpr (MASKED) {          // a masked key's weight is 0, but 0 times infinity is not
-          unclean = unclean || bad_pair(a[0].x) || bad_pair(a[0].y) || bad_pair(a[1].x) || bad_pair(a[1].y);
-          a[0] = make_uint2(finite_pair(a[0].x), finite_pair(a[0].y));
-          a[1] = make_uint2(finite_pair(a[1].x), finite_pair(a[1].y));
-        }
-        const uint4 both = make_uint4(a[0].x, a[0].y, a[1].x, a[1].y);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), w[u], o[d],
-                                                       0, 0, 0);
-      }
+      top = highest(n);
     }
-    if constexpr (MASKED) {
-      if (!__any(unclean)) return;
-      // Rare: the infinities and NaN of the keys that a row does see.
-#pragma unroll 1
-      for (int key = 0; key < kKeyTile; ++key) {
-        const int i = key & 15;
-        const bool seen = kt * kKeyTile + key < sees;
+    top = fmaxf(top, other_half(top));
+    if (!__any(fmaf(top, scale, -less) > kLazy) && !far) return;
+    // The reference moves by whole numbers, so the factor is a power of two and exact in bf16 too.
+    const float c_top = top * scale;
+    const bool up = is_far ? (top - m) * scale > kLazy : c_top - less > kLazy;
+    const bool now_far = up ? !(fabsf(c_top) <= kFar) : is_far;
+    const float raised = up && !now_far ? ceilf(c_top) : less;
+    const float f = !up ? 1.0f
+                        : exp2f(is_far ? (m - top) * scale : less - (now_far ? c_top : raised));
+    if (up) m = top;
+    is_far = now_far;
+    less = is_far ? 0.0f : raised;
+    far = __any(is_far);
+    l *= f;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int dim = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
-            const uint32_t x = *reinterpret_cast<const uint16_t*>(
-                kv + kTileBytes + key * (D * 2) + slot(i, dim / 8) * 16 + (dim % 8) * 2);
-            if (seen && (x & 0x7f80u) == 0x7f80u) o[d][e] += mrg::bf16_lo(x);
-          }
+      for (int i = 0; i < 16; ++i) o[d][i] *= f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x2 both = {(__bf16)(mrg::bf16_lo(w[u][i]) * f), (__bf16)(mrg::bf16_hi(w[u][i]) * f)};
+        w[u][i] = __builtin_bit_cast(uint32_t, both);
       }
+    if (is_far) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) n[i] -= m;
     }
+  };
+  // Weights i and i + 1 of scores s, computed here and not where they are used next (they are kept as 8
+  // registers, not the 16 that they are rounded from, and between the matrix instructions).
+  auto weigh = [&](const f32x16& s, int i, u32x4 (&w)[2]) __attribute__((always_inline)) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -less));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], scale, -less));
+    const bf16x2 both = {(__bf16)e0, (__bf16)e1};
+    uint32_t bits = __builtin_bit_cast(uint32_t, both);
+    l += e0;
+    l += e1;
+    asm volatile("" : "+v"(bits), "+v"(l));
+    w[i / 8][i % 8 / 2] = bits;
+  };
+  auto score_part = [&](const bf16x8& a, int i, f32x16& n) __attribute__((always_inline)) {
+    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], n, 0, 0, 0);
+  };
+  auto product_part = [&](const bf16x8& a, int i, const u32x4 (&w)[2]) __attribute__((always_inline)) {
+    o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        a, __builtin_bit_cast(bf16x8, w[(i - 8) >> 2]), o[i & 3], 0, 0, 0);
+  };
+  // Unit `unit` of a step: the scores of the next step's unit (K at ka), the weights of the scores s, and the
+  // product of the older weights w (V at va), none of which waits for another: 16 matrix instructions with
+  // the vector instructions of one weight each between them, and the LDS reads kRing - 1 ahead.
+  auto pipeline = [&](int unit, bf16x8 (&ring)[kRing], const f32x16& s, const u32x4 (&w)[2],
+                      u32x4 (&now)[2], f32x16& n) __attribute__((always_inline)) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int ahead = 16 * unit + i + kRing - 1;
+      if (ahead < 32) ring[(i + kRing - 1) % kRing] = fragment(ahead / 16, ahead % 16);
+      if (i < 8)
+        score_part(ring[i % kRing], i, n);
+      else
+        product_part(ring[i % kRing], i, w);
+      if (i % 2 == 0) weigh(s, i, now);
+      if (i == 10) top = fmaxf(n[0], n[1]);
+      if (i >= 10 && i < 15)
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (2 + 3 * (i - 10) + j < 16) top = fmaxf(top, n[2 + 3 * (i - 10) + j]);
+      if (i == 14) asm volatile("" : "+v"(top));     // here, not behind the branches
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return top;
   };
 
   if (k0 < k1) {
-    int bad = stage(entries(k0), 0), bad_now = 0, kt = k0;
-    Pages next = entries(k0 + 1);
-    // Waits for step kt and requests the next one; returns the keys.
-    auto advance = [&]() -> const unsigned char* {
-      const int buffer = (kt - k0) & 1;
-      bad_now = bad;
-      arrived();                         // the step's keys are here, and the last step's reads are done
-      if (kt + 1 < k1) {
-        bad = stage(next, 1 - buffer);
-        next = entries(kt + 2);
+    // K runs a step ahead of V: the wait for step kt is for K of kt + 1 and V of kt, and behind it K of
+    // kt + 2 and V of kt + 1 are requested.
+    int bad0 = 0, bad1 = 0, bad2 = 0;                // of steps kt, kt + 1, kt + 2
+    int kt = k0, to = 0;                             // to: the buffer of kt
+    int page = my_page(entries(kt), bad0);           // this wavefront's, of the K requested last
+    load_k(page, 0);
+    load_v(page, 0);
+    if (kt + 1 < k1) {
+      page = my_page(entries(kt + 1), bad1);
+      load_k(page, kBufferBytes);
+    }
+    Pages next = entries(kt + 2);
+    if (threadIdx.x == 0) s_found = 0;
+    arrived();
+    f32x16 s, n;
+    u32x4 w[2] = {}, now[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = n[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) score_part(fragment(0, i), i, s);
+    take(s, highest(s), w, kt * kKeyTile, bad0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) score_part(fragment(1, i), i, n);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) weigh(s, i, w);
+    take(n, highest(n), w, kt * kKeyTile + kUnit, bad0 >> 2);
+    s = n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ka[i] ^= kBufferBytes;
+    for (; kt + 1 < k1; ++kt) {
+      arrived();                                     // K of kt + 1 and V of kt; older units are read
+      load_v(page, to ^ kBufferBytes);
+      bad2 = 0;
+      if (kt + 2 < k1) {
+        page = my_page(next, bad2);
+        load_k(page, to);
+        next = entries(kt + 3);
       }
-      return s_kv + buffer * 2 * kTileBytes;
-    };
-    while (kt < k1) {
-      for (; kt < k1 && (kt + 1) * kKeyTile <= all_see && bad == 0; ++kt) {
-        const unsigned char* const kv = advance();
-        step(std::false_type{}, kt, kv, 0);
+      if (kt >= edge) clean(to);
+      bf16x8 ring[kRing];
+#pragma unroll
+      for (int i = 0; i < kRing - 1; ++i) ring[i] = fragment(0, i);
+      float top = pipeline(0, ring, s, w, now, n);
+      take(n, top, now, (kt + 1) * kKeyTile, bad1);
+      top = pipeline(1, ring, n, now, w, s);
+      take(s, top, w, (kt + 1) * kKeyTile + kUnit, bad1 >> 2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ka[i] ^= kBufferBytes;
+        va[i] ^= kBufferBytes;
       }
-      if (kt == k1) break;
-      const unsigned char* const kv = advance();
-      step(std::true_type{}, kt, kv, bad_now);
-      ++kt;
+      bad1 = bad2;
+      to ^= kBufferBytes;
+    }
+    arrived();
+    if (kt >= edge) clean(to);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) weigh(s, i, now);
+#pragma unroll
+    for (int i = 8; i < 16; ++i) product_part(fragment(0, i), i, w);
+#pragma unroll
+    for (int i = 8; i < 16; ++i) product_part(fragment(1, i), i, now);
+
+    if (s_found != 0) {                              // infinities and NaN among the keys from `edge` on
+#pragma unroll 1
+      for (int pos = edge * kKeyTile; pos < min(keys, k1 * kKeyTile); ++pos) {
+        const int entry = bt ? bt[pos / P] : b * p.max_pages + pos / P;
+        if ((unsigned)entry >= (unsigned)p.num_pages) continue;    // its scores are NaN
+        const uint16_t* const x = p.v + entry * page_stride + head_off + (pos % P) * D + 4 * half;
+        if (pos >= sees) continue;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t v = x[32 * d + 8 * (i / 4) + i % 4];
+            if ((v & 0x7f80u) == 0x7f80u) o[d][i] += mrg::bf16_lo(v);
+          }
+      }
     }
   }
 
@@ -381,7 +474,7 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
   if (!live) return;
   const bool empty = l == 0.0f;          // no position, or every score -inf
   const float inv = empty ? 0.0f : 1.0f / l;
-  const float lse = poison ? NAN : empty ? -INFINITY : (cm + log2f(l)) * kLn2;
+  const float lse = poison ? NAN : empty ? -INFINITY : ((is_far ? m * scale : less) + log2f(l)) * kLn2;
   if (p.part_o != nullptr) {
     const int64_t at = (out_row * p.splits + split) * p.hq + h;
     if (half == 0) p.part_lse[at] = lse;
@@ -403,7 +496,7 @@ __global__ void __launch_bounds__(64 * W, 2) rows_attn_kernel(const RowsParams p
       for (int a = 0; a < 4; ++a) {
         float x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = poison ? NAN : o[d][4 * a + j] * inv;
+        for (int j = 0; j < 4; ++j) x[j] = poison ? NAN : empty ? 0.0f : o[d][4 * a + j] * inv;
         dst[8 * d + 2 * a + half] = make_uint2(mrg::bf16_rne(x[0]) | (mrg::bf16_rne(x[1]) << 16),
                                                mrg::bf16_rne(x[2]) | (mrg::bf16_rne(x[3]) << 16));
       }
