@@ -29,6 +29,7 @@
 #include "linear_mfma.h"
 #include "merge_body.h"
 #include "qf_internal.h"
+#include "rows_body.h"
 
 namespace qf {
 namespace {
@@ -239,6 +240,17 @@ __device__ __forceinline__ ShardRange shard_range(const int32_t* __restrict__ ct
   return r;
 }
 
+// A workgroup's LDS in sweep_unit: the matrix path's K tiles, and where the wavefronts' states meet.
+template <int G, int W>
+struct SweepLds {
+  static constexpr bool MF = G >= 4;
+  uint4 k[MF ? W : 1][MF ? P * 16 : 1];
+  float acc[W][G][D];
+  float m[W][G];
+  float l[W][G];
+  int bad[W];
+};
+
 // The sweep of one unit by one workgroup; `bid` plays the role of the workgroup index (it is the
 // index itself in decode_split_kernel, the sweep's share of the indices in a shared launch).
 // With MERGE, the unit also takes part in the fused merge (merge_if_last).
@@ -250,7 +262,7 @@ __device__ __forceinline__ void sweep_unit(
     float* __restrict__ out_o, float* __restrict__ out_lse, int32_t hq, int32_t hkv,
     int32_t max_pages, int32_t num_pages, int32_t max_shards, int32_t chunks, int32_t n_units,
     int32_t batch, int32_t run, UnitDivisors by, float scale_log2, const unsigned bid,
-    int32_t* __restrict__ counters = nullptr, uint16_t* __restrict__ merged_o = nullptr,
+    SweepLds<G, W>& lds, int32_t* __restrict__ counters = nullptr, uint16_t* __restrict__ merged_o = nullptr,
     float* __restrict__ merged_lse = nullptr, const int32_t* __restrict__ unit_order = nullptr,
     int32_t counter_step = 1) {
   // Which unit this workgroup sweeps.  Workgroups are dispatched in index order, round-robin over
@@ -457,7 +469,7 @@ __device__ __forceinline__ void sweep_unit(
   // 4i + row (i = 0..3), the very positions whose V this lane reads, for head col % G.  Four
   // v_mfma_f32_16x16x32_bf16 (exact bf16 products, fp32 sums) replace 4G dot products and 4G
   // 16-lane reductions per position quad.
-  __shared__ uint4 s_k[MF ? W : 1][MF ? P * 16 : 1];
+  auto& s_k = lds.k;
   auto process_mf = [&](uint4* kc, uint4* vc, int pg) {
     const int valid = n - pg * P;  // slots [0, valid) of this page are cached positions
     uint4* tile = s_k[wave];
@@ -612,10 +624,10 @@ __device__ __forceinline__ void sweep_unit(
   // Merge the 4 rows of the wavefront (lanes col, col+16, col+32, col+48 hold the same dims), by
   // swapping registers between rows: the sums of 8 dims take 4 row swaps and 2 half swaps, and leave
   // each row with 2 of them (rows 0..3: dims 0-1, 4-5, 2-3, 6-7), each (r0 + r1) + (r2 + r3).
-  __shared__ float s_acc[W][G][D];
-  __shared__ float s_m[W][G];
-  __shared__ float s_l[W][G];
-  __shared__ int s_bad[W];
+  auto& s_acc = lds.acc;
+  auto& s_m = lds.m;
+  auto& s_l = lds.l;
+  auto& s_bad = lds.bad;
 #pragma unroll
   for (int h = 0; h < G; ++h) {
     float M = m[h], x, y;
@@ -717,9 +729,10 @@ decode_split_kernel(const uint16_t* __restrict__ qp, const uint16_t* __restrict_
                     int32_t hkv, int32_t max_pages, int32_t num_pages, int32_t max_shards,
                     int32_t chunks, int32_t n_units, int32_t batch, int32_t run, UnitDivisors by,
                     float scale_log2, const int32_t* __restrict__ unit_order) {
+  __shared__ SweepLds<G, W> lds;
   sweep_unit<G, W, NBUF>(qp, kp, vp, block_table, ctx_lens, n_shards, out_o, out_lse, hq, hkv,
                          max_pages, num_pages, max_shards, chunks, n_units, batch, run, by,
-                         scale_log2, blockIdx.x, nullptr, nullptr, nullptr, unit_order);
+                         scale_log2, blockIdx.x, lds, nullptr, nullptr, nullptr, unit_order);
 }
 
 // The XCD dealing cycle of rank_units_kernel: kXcdWeightEven : kXcdWeightOdd in lowest terms
@@ -914,9 +927,10 @@ decode_fused_kernel(const uint16_t* __restrict__ qp, const uint16_t* __restrict_
                     float scale_log2, int32_t* __restrict__ counters,
                     uint16_t* __restrict__ merged_o, float* __restrict__ merged_lse,
                     int32_t counter_step) {
+  __shared__ SweepLds<G, W> lds;
   sweep_unit<G, W, NBUF, true>(qp, kp, vp, block_table, ctx_lens, n_shards, out_o, out_lse, hq,
                                hkv, max_pages, num_pages, max_shards, chunks, n_units,
-                               batch, run, by, scale_log2, blockIdx.x, counters,
+                               batch, run, by, scale_log2, blockIdx.x, lds, counters,
                                merged_o, merged_lse, nullptr, counter_step);
 }
 
@@ -986,10 +1000,11 @@ sweep_beside_linear_kernel(
   const unsigned long long S = (unsigned)units_per_xcd, T = S + (unsigned)linear_groups;
   const unsigned before = (unsigned)(j * S / T);          // sweep groups dealt before group j
   if ((unsigned)((j + 1ull) * S / T) > before) {
+    __shared__ SweepLds<G, kSplitWaves> lds;
     sweep_unit<G, kSplitWaves, kSplitBuffers>(qp, kp, vp, block_table, ctx_lens, n_shards, out_o,
                                               out_lse, hq, hkv, max_pages, num_pages, max_shards,
                                               chunks, n_units, batch, run, by,
-                                              scale_log2, 8u * before + lane8, nullptr, nullptr,
+                                              scale_log2, 8u * before + lane8, lds, nullptr, nullptr,
                                               nullptr, unit_order);
     return;
   }
@@ -1115,6 +1130,36 @@ hipError_t launch_beside_g(const SplitParams& p, const LinearParams& l, hipStrea
   }
 }
 
+// One launch, two roles: the rows of shared prefixes (rows_body.h) first, then the sweep of the requests'
+// own positions.  The prefixes' workgroups live long and are bound by the matrix cores, the sweep's are
+// short and stream; the latter take the room beside the former and behind them.
+template <int G>
+__global__ void __launch_bounds__(64 * kSplitWaves, 2)
+rows_beside_sweep_kernel(const RowsParams r, const SplitParams p, const int32_t row_items) {
+  static_assert(rows::W == kSplitWaves, "both roles use the same workgroup size");
+  union Lds {
+    rows::Lds rows;
+    SweepLds<G, kSplitWaves> sweep;
+  };
+  __shared__ Lds lds;
+  if ((int)blockIdx.x < row_items) {
+    if ((int)blockIdx.x < r.slots * r.hkv) rows::item(r, blockIdx.x, lds.rows);
+    return;
+  }
+  sweep_unit<G, kSplitWaves, kSplitBuffers>(p.q, p.k, p.v, p.block_table, p.ctx_lens, p.n_shards, p.out_o,
+                                            p.out_lse, p.hq, p.hkv, p.max_pages, p.num_pages,
+                                            p.max_shards, p.chunks, p.n_units, p.batch, p.run, p.by,
+                                            p.scale_log2, blockIdx.x - (unsigned)row_items, lds.sweep);
+}
+
+template <int G>
+hipError_t launch_rows_beside_g(const RowsParams& r, const SplitParams& p, hipStream_t stream) {
+  const unsigned row_items = ((unsigned)r.slots * (unsigned)r.hkv + 7u) / 8u * 8u;   // keeps indices mod 8
+  hipLaunchKernelGGL((rows_beside_sweep_kernel<G>), dim3(row_items + 8u * (unsigned)p.units_per_xcd),
+                     dim3(64 * kSplitWaves), 0, stream, r, p, (int32_t)row_items);
+  return hipGetLastError();
+}
+
 // Workgroups of the two-buffer kernel that the chunk rule counts as resident per compute unit: those of
 // the kernel's earlier register counts, which the rule was measured with (per-GPU share of a 2^20
 // request, 1,024 instead of 768 at G = 2: 90.4 -> 91.3 us, more workgroups in flight only add
@@ -1170,6 +1215,17 @@ hipError_t launch_decode_split_beside(const SplitParams& p, int group, const Lin
     case 2: return launch_beside_g<2>(p, l, stream);
     case 4: return launch_beside_g<4>(p, l, stream);
     case 8: return launch_beside_g<8>(p, l, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_rows_beside_sweep(const RowsParams& r, const SplitParams& p, int group,
+                                    hipStream_t stream) {
+  switch (group) {
+    case 1: return launch_rows_beside_g<1>(r, p, stream);
+    case 2: return launch_rows_beside_g<2>(r, p, stream);
+    case 4: return launch_rows_beside_g<4>(r, p, stream);
+    case 8: return launch_rows_beside_g<8>(r, p, stream);
     default: return hipErrorInvalidValue;
   }
 }

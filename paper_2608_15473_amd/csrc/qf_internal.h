@@ -158,13 +158,14 @@ struct RowsParams {
   const int32_t* block_table;   // [seqs, max_pages] or null (identity)
   const int32_t* ctx_lens;      // [seqs]
   const int32_t* cu;            // [seqs + 1]
-  uint16_t* out;                // bf16 [rows, Hq, D], with part_o null
-  float* lse;                   // fp32 [rows, Hq] or null
-  float* part_o;                // fp32 [rows, splits, Hq, D] or null
-  float* part_lse;              // fp32 [rows, splits, Hq]
+  uint16_t* out;                // bf16 [rows, Hq, D]: of tiles with one key range; null: none is
+  float* lse;                   // fp32 [rows, Hq] or null, likewise
+  float* part_o;                // fp32 [rows, entries, Hq, D], with entries > 1 or out null
+  float* part_lse;              // fp32 [rows, entries, Hq]
+  int32_t* range;               // written: steps of a key range; with part_o
   int32_t seqs, rows, hq, hkv, max_pages, num_pages;
-  int32_t tiles;                // bound on the row tiles of one KV head (rows_tiles)
-  int32_t splits;               // ranges that a tile's keys are cut into
+  int32_t slots;                // work items of a KV head, at least its row tiles
+  int32_t entries;              // most ranges that a tile's keys are cut into
   bool causal;
   float scale_log2;             // softmax scale * log2(e)
 };
@@ -176,18 +177,20 @@ inline int64_t rows_tiles(int64_t rows, int64_t group, int64_t seqs) {
 }
 hipError_t launch_rows_attn(const RowsParams& p, hipStream_t stream);
 
-// The pairs of one or two sources joined per (row, head): rows of no sequence of `cu` have no pairs in
-// the first source, and are not written where there is no second.
+// The pairs of one or two sources joined per (row, head): the first those that launch_rows_attn left (none
+// for rows of no sequence of `cu`); without a second, only rows of several pairs are written.
 struct JoinParams {
   const float* a_o;             // fp32 [rows, a_entries, Hq, D]
   const float* a_lse;
   const float* b_o;             // fp32 [rows, b_entries, Hq, D]
   const float* b_lse;
-  const int32_t* cu;            // [seqs + 1]
+  const int32_t* cu;            // as launch_rows_attn had them, and the range that it wrote
+  const int32_t* ctx_lens;
+  const int32_t* range;
   void* out;                    // bf16 [rows, Hq, D], or fp32 with `pair`
   float* lse;                   // fp32 [rows, Hq] or null
-  int32_t seqs, rows, hq, a_entries, b_entries;   // b_entries == 0: no second source
-  bool pair;
+  int32_t seqs, rows, hq, hkv, max_pages, a_entries, b_entries;   // b_entries == 0: no second source
+  bool causal, pair;
 };
 hipError_t launch_join(const JoinParams& p, hipStream_t stream);
 
@@ -222,6 +225,10 @@ constexpr int kCounterStep = 32;
 // The sweep and a fused product in one launch (decode_split.hip).
 hipError_t launch_decode_split_beside(const SplitParams& p, int group, const LinearParams& l,
                                       hipStream_t stream);
+
+// The rows of shared prefixes and the sweep of the requests' own positions in one launch (decode_split.hip).
+hipError_t launch_rows_beside_sweep(const RowsParams& r, const SplitParams& p, int group,
+                                    hipStream_t stream);
 
 // Host simulation of the layer-wise decode schedule (schedule.cpp).
 int simulate_schedule(int R, const double* arrival, const double* attn_time, int L, int wiring,

@@ -283,25 +283,62 @@ int finish_split(const Split& sp, hipStream_t s) {
 // Workgroups of one launch: a grid's work items are counted in 32 bits, at 256 a workgroup.
 constexpr int64_t kMaxGrid = (1 << 24) - 1;
 
-// Ranges that every row tile's keys are cut into: one, or, where there are fewer tiles than the chip keeps
-// resident (two workgroups a compute unit), as many as fill it, each of kMinKeySteps steps at least at the
-// table's capacity.  They depend on the shape alone, so a shape always has the same sums.
+// Work items of a KV head: its row tiles, or, where there are fewer than the chip keeps resident (two
+// workgroups a compute unit), as many as that, the tiles' keys being cut into ranges.  `entries` is the most
+// that one tile's may be cut into: what the items leave room for beside the other tiles, the
+// steps of a full table, kMostEntries, and kPairBytes of pairs (4 ranges at least).
 constexpr int64_t kRowsResident = 512;
-constexpr int64_t kMinKeySteps = 4;
-int64_t rows_splits(int64_t tiles, int64_t hkv, int64_t max_pages) {
+constexpr int64_t kMostEntries = 64;
+constexpr int64_t kPairBytes = 128 << 20;
+struct Items {
+  int64_t slots = 0, entries = 1;
+};
+Items rows_items(int64_t rows, int64_t hq, int64_t hkv, int64_t seqs, int64_t max_pages) {
   const int64_t steps = (max_pages * qf::kPage + qf::kKeyTile - 1) / qf::kKeyTile;
-  return std::max<int64_t>(1, std::min(kRowsResident / std::max<int64_t>(1, tiles * hkv),
-                                       steps / kMinKeySteps));
+  const int64_t full = rows * (hq / hkv) / qf::kRowsTile;
+  const int64_t in_bytes = kPairBytes / (rows * hq * (qf::kHeadDim + 1) * (int64_t)sizeof(float));
+  Items it;
+  it.slots = qf::rows_tiles(rows, hq / hkv, seqs);
+  if (it.slots >= kRowsResident / hkv) return it;
+  it.entries = std::max<int64_t>(1, std::min({kRowsResident / hkv - full + 1, steps, kMostEntries,
+                                              std::max<int64_t>(4, in_bytes)}));
+  if (it.entries > 1) it.slots = kRowsResident / hkv;
+  return it;
 }
 
-// The floats of pairs [rows, entries, Hq, D + 1], the vectors first, rounded up to 16 bytes.
+// The floats of pairs [rows, entries, Hq, D + 1], the vectors first, and a word for the range that was
+// taken, rounded up to 16 bytes.
 size_t pair_floats(int64_t rows, int64_t entries, int64_t hq) {
-  return ((size_t)rows * entries * hq * (qf::kHeadDim + 1) + 3) / 4 * 4;
+  return ((size_t)rows * entries * hq * (qf::kHeadDim + 1) + 1 + 3) / 4 * 4;
+}
+
+// The pairs of p's rows in the workspace, and what joins them.
+void place_pairs(qf::RowsParams* p, void* workspace) {
+  const size_t pairs = (size_t)p->rows * p->entries * p->hq;
+  p->part_o = static_cast<float*>(workspace);
+  p->part_lse = p->part_o + pairs * qf::kHeadDim;
+  p->range = reinterpret_cast<int32_t*>(p->part_lse + pairs);
+}
+qf::JoinParams join_of(const qf::RowsParams& p) {
+  qf::JoinParams j{};
+  j.a_o = p.part_o;
+  j.a_lse = p.part_lse;
+  j.cu = p.cu;
+  j.ctx_lens = p.ctx_lens;
+  j.range = p.range;
+  j.seqs = p.seqs;
+  j.rows = p.rows;
+  j.hq = p.hq;
+  j.hkv = p.hkv;
+  j.max_pages = p.max_pages;
+  j.a_entries = p.entries;
+  j.causal = p.causal;
+  return j;
 }
 
 struct Prefill {
-  int64_t tiles, splits;
-  size_t bytes;
+  Items items;
+  size_t bytes = 0;
 };
 int plan_prefill(const qf_decode_desc* desc, int32_t n_tokens, Prefill* pl) {
   const int rc = check_desc(desc);
@@ -311,23 +348,23 @@ int plan_prefill(const qf_decode_desc* desc, int32_t n_tokens, Prefill* pl) {
   if ((int64_t)n_tokens * group > INT32_MAX - qf::kRowsTile)
     return fail(QF_EINVAL, "n_tokens %d too large", n_tokens);
   if (desc->batch == 0 || n_tokens == 0) {
-    *pl = Prefill{0, 1, 0};
+    *pl = Prefill{};
     return QF_OK;
   }
-  pl->tiles = qf::rows_tiles(n_tokens, group, desc->batch);
-  pl->splits = rows_splits(pl->tiles, desc->n_kv_heads, desc->max_pages_per_seq);
-  pl->bytes = pl->splits > 1
-                  ? pair_floats(n_tokens, pl->splits, desc->n_q_heads) * sizeof(float) : 0;
+  pl->items = rows_items(n_tokens, desc->n_q_heads, desc->n_kv_heads, desc->batch, desc->max_pages_per_seq);
+  pl->bytes = pl->items.entries > 1
+                  ? pair_floats(n_tokens, pl->items.entries, desc->n_q_heads) * sizeof(float) : 0;
   // The most workgroups of a launch, and the rows of the join.
-  if (pl->tiles * pl->splits * desc->n_kv_heads > kMaxGrid ||
-      (pl->splits > 1 && (int64_t)n_tokens * desc->n_q_heads > kMaxGrid))
+  if (pl->items.slots * desc->n_kv_heads > kMaxGrid ||
+      (pl->items.entries > 1 && (int64_t)n_tokens * desc->n_q_heads > kMaxGrid))
     return fail(QF_EINVAL, "too many row tiles for one launch (%d tokens)", n_tokens);
   return QF_OK;
 }
 
 struct Shared {
-  int64_t tiles, splits, slots;       // slots: shards x chunks of the requests' own positions
-  size_t prefix_floats, bytes;
+  Items items;                        // of the prefixes
+  int64_t slots = 0;                  // shards x chunks of the requests' own positions
+  size_t prefix_floats = 0, bytes = 0;
 };
 int plan_shared(const qf_decode_desc* desc, int32_t n_groups, int32_t max_prefix_pages, Shared* pl) {
   const int rc = check_desc(desc);
@@ -336,18 +373,17 @@ int plan_shared(const qf_decode_desc* desc, int32_t n_groups, int32_t max_prefix
   if (n_groups < 0) return fail(QF_EINVAL, "n_groups %d < 0", n_groups);
   if (n_groups > 0 && (max_prefix_pages < 1 || (int64_t)max_prefix_pages * qf::kPage > INT32_MAX))
     return fail(QF_EINVAL, "max_prefix_pages %d out of range", max_prefix_pages);
-  const int64_t group = d.n_q_heads / d.n_kv_heads;
   if ((int64_t)d.batch * d.n_q_heads > kMaxGrid)
     return fail(QF_EINVAL, "batch * n_q_heads too large");
-  *pl = Shared{0, 1, 0, 0, 0};
+  *pl = Shared{};
   if (d.batch == 0) return QF_OK;
   pl->slots = d.max_shards * choose_chunks(&d);
   if (pl->slots > INT32_MAX) return fail(QF_EINVAL, "max_shards * chunks exceeds int32");
   if (n_groups > 0) {
-    pl->tiles = qf::rows_tiles(d.batch, group, n_groups);
-    pl->splits = rows_splits(pl->tiles, d.n_kv_heads, max_prefix_pages);
-    pl->prefix_floats = pair_floats(d.batch, pl->splits, d.n_q_heads);
-    if (pl->tiles * pl->splits * d.n_kv_heads > kMaxGrid)
+    pl->items = rows_items(d.batch, d.n_q_heads, d.n_kv_heads, n_groups, max_prefix_pages);
+    pl->prefix_floats = pair_floats(d.batch, pl->items.entries, d.n_q_heads);
+    const int64_t units = (int64_t)d.batch * pl->slots * d.n_kv_heads;
+    if (pl->items.slots * d.n_kv_heads + units + units / 8 + 64 > kMaxGrid)
       return fail(QF_EINVAL, "too many row tiles for one launch (%d requests)", d.batch);
   }
   pl->bytes = (pl->prefix_floats + pair_floats(d.batch, pl->slots, d.n_q_heads)) * sizeof(float);
@@ -1040,30 +1076,19 @@ int qf_attn_prefill(const qf_decode_desc* desc, int32_t n_tokens, const void* q,
   p.hkv = d.n_kv_heads;
   p.max_pages = d.max_pages_per_seq;
   p.num_pages = d.num_pages;
-  p.tiles = (int32_t)pl.tiles;
-  p.splits = (int32_t)pl.splits;
+  p.slots = (int32_t)pl.items.slots;
+  p.entries = (int32_t)pl.items.entries;
   p.causal = true;
   p.scale_log2 = (float)((double)d.softmax_scale * 1.4426950408889634);
-  if (pl.splits > 1) {
-    p.part_o = static_cast<float*>(workspace);
-    p.part_lse = p.part_o + (size_t)n_tokens * pl.splits * d.n_q_heads * qf::kHeadDim;
-  } else {
-    p.out = static_cast<uint16_t*>(out);
-    p.lse = lse;
-  }
+  p.out = static_cast<uint16_t*>(out);
+  p.lse = lse;
+  if (p.entries > 1) place_pairs(&p, workspace);
   hipError_t e = qf::launch_rows_attn(p, s);
   if (e != hipSuccess) return fail(QF_EHIP, "prefill launch: %s", hipGetErrorString(e));
-  if (pl.splits == 1) return QF_OK;
-  qf::JoinParams j{};
-  j.a_o = p.part_o;
-  j.a_lse = p.part_lse;
-  j.cu = cu_tokens;
+  if (p.entries == 1) return QF_OK;
+  qf::JoinParams j = join_of(p);
   j.out = out;
   j.lse = lse;
-  j.seqs = d.batch;
-  j.rows = n_tokens;
-  j.hq = d.n_q_heads;
-  j.a_entries = p.splits;
   e = qf::launch_join(j, s);
   if (e != hipSuccess) return fail(QF_EHIP, "prefill join launch: %s", hipGetErrorString(e));
   return QF_OK;
@@ -1100,8 +1125,7 @@ int qf_attn_decode_shared(const qf_decode_desc* desc, const void* q, const void*
     return fail(QF_EALIGN, "workspace and a pair's out must be 16-byte aligned, the others 4-byte");
   if (workspace_size < pl.bytes)
     return fail(QF_EINVAL, "workspace of %zu bytes < %zu needed", workspace_size, pl.bytes);
-  float* const prefix_o = static_cast<float*>(workspace);
-  float* const own_o = prefix_o + pl.prefix_floats;
+  float* const own_o = static_cast<float*>(workspace) + pl.prefix_floats;
   float* const own_lse = own_o + (size_t)d.batch * pl.slots * d.n_q_heads * qf::kHeadDim;
   Split sp;
   rc = prepare_split(desc, q, k_cache, v_cache, block_table, ctx_lens, n_shards, own_o, own_lse,
@@ -1109,6 +1133,7 @@ int qf_attn_decode_shared(const qf_decode_desc* desc, const void* q, const void*
   if (rc || sp.noop) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   qf::JoinParams j{};
+  hipError_t e = hipSuccess;
   if (n_groups > 0) {
     qf::RowsParams p{};
     p.q = static_cast<const uint16_t*>(q);
@@ -1117,35 +1142,31 @@ int qf_attn_decode_shared(const qf_decode_desc* desc, const void* q, const void*
     p.block_table = prefix_table;
     p.ctx_lens = prefix_lens;
     p.cu = group_rows;
-    p.part_o = prefix_o;
-    p.part_lse = prefix_o + (size_t)d.batch * pl.splits * d.n_q_heads * qf::kHeadDim;
     p.seqs = n_groups;
     p.rows = d.batch;
     p.hq = d.n_q_heads;
     p.hkv = d.n_kv_heads;
     p.max_pages = max_prefix_pages;
     p.num_pages = d.num_pages;
-    p.tiles = (int32_t)pl.tiles;
-    p.splits = (int32_t)pl.splits;
+    p.slots = (int32_t)pl.items.slots;
+    p.entries = (int32_t)pl.items.entries;
     p.causal = false;
     p.scale_log2 = (float)((double)d.softmax_scale * 1.4426950408889634);
-    const hipError_t e = qf::launch_rows_attn(p, s);
-    if (e != hipSuccess) return fail(QF_EHIP, "prefix launch: %s", hipGetErrorString(e));
-    j.a_o = p.part_o;
-    j.a_lse = p.part_lse;
-    j.a_entries = p.splits;
+    place_pairs(&p, workspace);
+    e = qf::launch_rows_beside_sweep(p, sp.p, sp.group, s);
+    j = join_of(p);
+  } else {
+    e = qf::launch_decode_split(sp.p, sp.group, s);
   }
-  hipError_t e = qf::launch_decode_split(sp.p, sp.group, s);
-  if (e != hipSuccess) return fail(QF_EHIP, "decode_split launch: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return fail(QF_EHIP, "decode_shared launch: %s", hipGetErrorString(e));
   j.b_o = own_o;
   j.b_lse = own_lse;
   j.b_entries = (int32_t)pl.slots;
-  j.cu = group_rows;
   j.out = out;
   j.lse = lse;
-  j.seqs = n_groups;
   j.rows = d.batch;
   j.hq = d.n_q_heads;
+  j.hkv = d.n_kv_heads;
   j.pair = pair != 0;
   e = qf::launch_join(j, s);
   if (e != hipSuccess) return fail(QF_EHIP, "join launch: %s", hipGetErrorString(e));

@@ -1,0 +1,703 @@
+// Attention of packed query rows over a paged grouped-query KV cache, on the matrix cores: the body of a
+// workgroup, shared by the launch of its own (rows_attn.hip) and the one that it shares with the sweep
+// (decode_split.hip).
+//
+// One pass over the keys: with s = q . k, c = scale * log2 e and a running reference r per row,
+//   p = exp2(c s - r),  l = sum p,  o = sum p v,  out = o / l,  lse = (r + log2 l) ln 2.
+// Where a score exceeds r by more than kLazy, r is raised to the next whole number above it, and what has
+// been summed is scaled by the power of two between (exact, in the bf16 weights too).  Past |r| = kFar
+// whole numbers are as coarse as fp32 scores: such rows keep the maximum m itself, p = exp2(c (s - m)).
+//
+// A workgroup takes one KV head and a tile of 128 query rows, a row being (token, query head of the
+// group), so that the G query heads of a KV head share every key read.  Its 4 wavefronts have 32 rows
+// each and step through the keys 64 (4 pages) at a time.  Scores are computed transposed,
+// S^T = K Q^T with v_mfma_f32_32x32x16_bf16, which leaves each lane 32 scores of ONE row (the other half
+// of the row's 64 in lane ^ 32): maximum and sum are in-lane.  The weights, rounded to bf16, are the B
+// operand of O^T = V^T P^T as they lie: the sum over keys may run in any order, so the keys of a step's
+// 16 are taken in the order in which the scores' layout has them, and V is read from LDS in that order,
+// transposed by ds_read_b64_tr_b16.  Rounding the weights to bf16 (2^-9 relative, to nearest, so errors
+// average out over the keys) is what the matrix cores take; l sums the unrounded weights in fp32.
+#pragma once
+
+#include <float.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "merge_body.h"
+#include "qf_internal.h"
+#include "row_owner.h"
+
+namespace qf {
+namespace rows {
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+constexpr int D = kHeadDim;
+constexpr int P = kPage;
+constexpr int W = 4;                     // wavefronts of a workgroup
+constexpr int kRowsPerWave = kRowsTile / W;
+constexpr int kPagesPerTile = kKeyTile / P;
+constexpr int kTileBytes = kKeyTile * D * 2;
+constexpr int kBufferBytes = 2 * kTileBytes;         // K and V of a step
+constexpr int kUnit = kKeyTile / 2;                  // keys that the pipeline takes at a time
+constexpr int kUnitBytes = kUnit * D * 2;
+constexpr int kRing = 4;                             // fragments in registers
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLazy = 8.0f;            // log2 units: p <= 256 between rescales
+constexpr float kFar = 1048576.0f;       // log2 units
+// The shortest range: one step per 32 rows of the fullest tile.  A row's pair is 516 bytes written and read
+// again, a step 32 KB, so full tiles would move more bytes for their pairs than for their keys below 4
+// steps (32 requests over 8,192 positions, G = 4: 14.6 us with 4, 16.6 with 3), few rows take the latency
+// of a range instead (4 requests over 1,531 positions, G = 2: 10.9 us with 4 steps, 7.3 with 1).
+__device__ __forceinline__ int least_range(int rows) { return (min(rows, kRowsTile) + 31) / 32; }
+static_assert(kPagesPerTile == W, "a wavefront stages one page of each step");
+
+typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
+
+// 16-byte slot, within the 16 of its row, of chunk ch (dims 8 ch .. 8 ch + 7) of row i of a page in LDS.
+// A row is 256 bytes, one round of the banks: the swizzle puts a chunk of 16 rows into 16 different
+// slots (the score operand's reads) and 4 neighbouring chunks of 4 rows too (the transposed reads).
+__device__ __forceinline__ int slot(int i, int ch) { return ch ^ (4 * (i & 3) + (i >> 2)); }
+
+// The other half-wavefront's value of x (lane ^ 32).
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// One page (4 KB) from global memory straight to LDS, by one wavefront: load j takes rows 4 j .. 4 j + 3,
+// lane l from page + 1024 j + (at ^ 16 j) to LDS byte to + 1024 j + 16 l.  Written as one block because the
+// compiler, which cannot tell the LDS buffers apart, would wait for the loads before every transposed read
+// of another buffer; whoever reads the page waits by hand (arrived()).  No output registers; M0 holds the
+// LDS base, which the loads may follow after one wait state (the compiler reserves M0 and sets it before
+// each use of its own).
+__device__ __forceinline__ void load_page(const void* page, int at, uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %5\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %0\n\t"
+      "global_load_lds_dwordx4 %2, %0 offset:1024\n\t"
+      "global_load_lds_dwordx4 %3, %0 offset:2048\n\t"
+      "global_load_lds_dwordx4 %4, %0 offset:3072"
+      :
+      : "s"(page), "v"(at), "v"(at ^ 16), "v"(at ^ 32), "v"(at ^ 48), "s"(to)
+      : "memory");
+}
+// Every load of this wavefront has arrived; then every wavefront's.
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Sequence b: its rows (none where they are out of order or range) and the positions before them.
+struct Sequence {
+  int start, len, before;
+  bool poison;                           // a length out of range: no position is read
+};
+__device__ __forceinline__ Sequence sequence(const int32_t* __restrict__ cu,
+                                             const int32_t* __restrict__ ctx_lens, int32_t rows,
+                                             int32_t max_pages, bool causal, int b) {
+  Sequence q{0, 0, 0, false};
+  const int s = cu[b], e = cu[b + 1], n = ctx_lens[b];
+  if (s < 0 || e <= s || e > rows) return q;
+  q.start = s;
+  q.len = e - s;
+  q.poison = n < 0 || (int64_t)n + (causal ? q.len : 0) > (int64_t)max_pages * P;
+  q.before = q.poison ? 0 : n;
+  return q;
+}
+// Positions that row `index` of it sees, and the steps of the tile whose first row (of len << gshift) is
+// `first`: those of its last row.
+__device__ __forceinline__ int sees_of(const Sequence& q, bool causal, int index) {
+  return q.poison ? 0 : causal ? q.before + index + 1 : q.before;
+}
+__device__ __forceinline__ int keys_of(const Sequence& q, bool causal, int gshift, int first) {
+  return sees_of(q, causal, min(first + kRowsTile - 1, (q.len << gshift) - 1) >> gshift);
+}
+__device__ __forceinline__ int steps_of(int keys) { return keys / kKeyTile + (keys % kKeyTile != 0); }
+__device__ __forceinline__ int tiles_of(const Sequence& q, int gshift) {
+  return (int)((((int64_t)q.len << gshift) + kRowsTile - 1) / kRowsTile);
+}
+// A tile's keys are cut into ranges of `range` steps.
+__device__ __forceinline__ int ranges_of(int steps, int range) { return steps > 0 ? (steps - 1) / range + 1 : 1; }
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
+  return x;
+}
+
+// What a workgroup does: rows first .. first + 127 of sequence seq, key range `part`.
+struct Work {
+  int seq, first, part, range;
+  Sequence q;
+};
+// Tiles of a causal sequence with at least n steps: from the first on whose last row sees more than
+// (n - 1) kKeyTile positions.
+__device__ __forceinline__ int tiles_from(const Sequence& q, int gshift, int tiles, int n) {
+  if (q.poison) return n <= 0 ? tiles : 0;
+  const int need = max(0, (n - 1) * kKeyTile - q.before);        // rows before the first such row
+  if (need >= q.len) return 0;
+  return tiles - (int)(((int64_t)need << gshift) / kRowsTile);
+}
+// The slot-th tile in order of length, the longest first, of causal sequences (a workgroup that starts late
+// has to be short): by bisection for its number of steps, then among the tiles of just that many.
+__device__ __forceinline__ Work longest_first(const RowsParams& p, int gshift, int slot) {
+  const int lane = threadIdx.x & 63;
+  auto each = [&](auto use) {            // every sequence, 64 at a time, one per lane
+    for (int b0 = 0; b0 < p.seqs; b0 += 64) {
+      Sequence q{0, 0, 0, false};
+      if (b0 + lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, true, b0 + lane);
+      if (use(b0, q)) return;
+    }
+  };
+  auto count = [&](int n) {              // tiles of at least n steps
+    int64_t sum = 0;
+    each([&](int, const Sequence& q) {
+      sum += tiles_from(q, gshift, tiles_of(q, gshift), n);
+      return false;
+    });
+    return wave_sum(sum);
+  };
+  int low = 0, high = (int)min((int64_t)p.max_pages * P / kKeyTile + 2, (int64_t)INT32_MAX);
+  if (p.seqs <= 64) {                    // the usual case: one sequence per lane, read once
+    Sequence q{0, 0, 0, false};
+    if (lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, true, lane);
+    const int t = tiles_of(q, gshift);
+    high = wave_max(t > 0 ? steps_of(sees_of(q, true, q.len - 1)) + 1 : 1);
+    while (high - low > 1) {             // count(low) > slot >= count(high), if slot has a tile at all
+      const int n = (low + high) / 2;
+      if (wave_sum((int64_t)tiles_from(q, gshift, t, n)) > slot) low = n; else high = n;
+    }
+  } else {
+    while (high - low > 1) {
+      const int n = (low + high) / 2;
+      if (count(n) > slot) low = n; else high = n;
+    }
+  }
+  int64_t before = count(low + 1);
+  Work w{-1, 0, 0, INT32_MAX, Sequence{0, 0, 0, false}};
+  each([&](int b0, const Sequence& q) {
+    const int t = tiles_of(q, gshift);
+    const int above = tiles_from(q, gshift, t, low + 1);
+    const int64_t items = tiles_from(q, gshift, t, low) - above;
+    int64_t upto = items;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t past = __ballot(before + upto > slot);
+    if (past == 0) {
+      before += __shfl(upto, 63);
+      return false;
+    }
+    const int l = __builtin_ctzll(past);
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    const int i = __builtin_amdgcn_readfirstlane(slot - (int)(before + __shfl(upto - items, l)));
+    w.seq = b0 + l;
+    w.first = (of(t) - of(above) - 1 - i) * kRowsTile;
+    w.q = Sequence{of(q.start), of(q.len), of(q.before), of(q.poison) != 0};
+    return true;
+  });
+  return w;
+}
+
+// Work item `slot` of a KV head; every wavefront finds it for itself, lane l looking at sequences l, l + 64, ...
+// The range is the least that leaves at most p.slots items and p.entries ranges a tile: with t tiles of n
+// steps each sequence has t ceil(n / range) of them.  Items of a range of keys lie side by side (their
+// tiles read the same keys).  Causal tiles without ranges differ in length: longest_first.
+__device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int slot) {
+  const int lane = threadIdx.x & 63;
+  int range = INT32_MAX;
+  if (p.seqs == 1) {                     // by scalar instructions alone
+    const Sequence q = sequence((const int32_t*)(const_i32_ptr)p.cu, (const int32_t*)(const_i32_ptr)p.ctx_lens,
+                                p.rows, p.max_pages, p.causal, 0);
+    const int t = tiles_of(q, gshift);
+    const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
+    if (p.entries > 1) {
+      const int64_t room = p.slots - t;
+      const int64_t r = room > 0 ? ((int64_t)t * n + room - 1) / room : INT32_MAX;
+      range = (int)min(max(max(r, (int64_t)((n + p.entries - 1) / p.entries)),
+                           (int64_t)least_range(q.len << gshift)), (int64_t)INT32_MAX);
+    }
+    const int parts = ranges_of(n, range);
+    if (slot >= t * parts) return Work{-1, 0, 0, range, q};
+    const int i = p.entries > 1 ? slot : t - 1 - slot;
+    return Work{0, i % t * kRowsTile, i / t, range, q};
+  }
+  if (p.entries > 1) {
+    int64_t all = 0, tiles = 0;
+    int longest = 0, most = 0;
+    for (int b0 = 0; b0 < p.seqs; b0 += 64) {
+      const int b = b0 + lane;
+      if (b < p.seqs) {
+        const Sequence q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, b);
+        const int t = tiles_of(q, gshift);
+        const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
+        all += (int64_t)t * n;
+        tiles += t;
+        longest = max(longest, n);
+        most = max(most, q.len << gshift);
+      }
+    }
+    all = wave_sum(all);
+    tiles = wave_sum(tiles);
+    longest = wave_max(longest);
+    most = wave_max(most);
+    const int64_t room = p.slots - tiles;
+    int64_t r = room > 0 ? (all + room - 1) / room : INT32_MAX;
+    r = max(r, (int64_t)((longest + p.entries - 1) / p.entries));
+    range = __builtin_amdgcn_readfirstlane((int)min(max(r, (int64_t)least_range(most)), (int64_t)INT32_MAX));
+  } else if (p.causal) {
+    return longest_first(p, gshift, slot);
+  }
+  int64_t before = 0;                    // items of the sequences before this round's
+  for (int b0 = 0; b0 < p.seqs; b0 += 64) {
+    const int b = b0 + lane;
+    Sequence q{0, 0, 0, false};
+    if (b < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, b);
+    const int t = tiles_of(q, gshift);
+    const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
+    const int64_t items = (int64_t)t * ranges_of(n, range);
+    int64_t upto = items;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t past = __ballot(before + upto > slot);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
+      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+      const int i = slot - (int)(before + __shfl(upto - items, l));
+      const int tl = of(t);
+      const int il = __builtin_amdgcn_readfirstlane(i);
+      return Work{b0 + l, il % tl * kRowsTile, il / tl, range,
+                  Sequence{of(q.start), of(q.len), of(q.before), of(q.poison) != 0}};
+    }
+    before += __shfl(upto, 63);
+  }
+  return Work{-1, 0, 0, range, Sequence{0, 0, 0, false}};
+}
+
+// A bf16 pair with zeros for infinities and NaN.
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+  return w;
+}
+
+// A workgroup's LDS: two steps' K and V, and whether V had infinities or NaN among masked steps.
+struct Lds {
+  alignas(1024) unsigned char kv[2 * kBufferBytes];
+  int found;
+};
+
+// Work item `item` of p (item % hkv: its KV head), by a whole workgroup.
+__device__ __forceinline__ void item(const RowsParams& p, const unsigned item, Lds& lds_mem) {
+  auto& s_kv = lds_mem.kv;
+  int& s_found = lds_mem.found;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5;
+  const int gshift = 31 - __builtin_clz(p.hq / p.hkv);
+
+  const int g = item % (unsigned)p.hkv;
+  const Work work = find_work(p, gshift, item / (unsigned)p.hkv);
+  if (item == 0 && threadIdx.x == 0 && p.range != nullptr) *p.range = work.range;
+  if (work.seq < 0) return;
+  const int b = work.seq;
+  const Sequence& seq = work.q;
+
+  // This lane's row: token and query head; rows past the sequence's repeat its last one.
+  const int n_rows = seq.len << gshift;
+  const int row = work.first + wave * kRowsPerWave + (lane & 31);
+  const bool live = row < n_rows;
+  const int index = (live ? row : n_rows - 1) >> gshift;
+  const int h = (g << gshift) + ((live ? row : n_rows - 1) & ((1 << gshift) - 1));
+  const int64_t out_row = (int64_t)seq.start + index;
+
+  // Positions that the row, every row of the wavefront, and some row of the tile sees.
+  const bool poison = seq.poison;
+  const int sees = sees_of(seq, p.causal, index);
+  const int all_see =
+      sees_of(seq, p.causal, min(work.first + wave * kRowsPerWave, n_rows - 1) >> gshift);
+  const int keys = keys_of(seq, p.causal, gshift, work.first);
+  const int steps = steps_of(keys);
+  const int parts = ranges_of(steps, work.range);
+  if (work.part >= parts) return;
+  const int k0 = work.part * work.range;             // no overflow: < steps, or part 0
+  const int k1 = (int)min((int64_t)k0 + work.range, (int64_t)steps);
+
+  // The queries: B operand of S^T, lane (half, row) holds dims 16 kk + 8 half .. + 7.  A negative scale
+  // is their sign; a zero one becomes 1e-37, so that scores of -inf stay -inf.
+  bf16x8 q[8];
+  {
+    const uint4* src = reinterpret_cast<const uint4*>(p.q + (out_row * p.hq + h) * D);
+    const uint32_t flip = p.scale_log2 < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      uint4 w = src[2 * kk + half];
+      w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
+      q[kk] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+  const float scale = fmaxf(fabsf(p.scale_log2), 1e-37f);
+
+  f32x16 o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  // The reference starts at the lowest finite value: no difference is inf - inf.
+  float m = -FLT_MAX, less = -FLT_MAX, l = 0.0f;   // less: the reference, 0 where m is it
+  bool is_far = false, far = false;      // m is, for this row, for some row of the wavefront
+
+  const int pages = (keys + P - 1) / P;
+  const const_i32_ptr bt =
+      p.block_table ? (const_i32_ptr)(p.block_table + (int64_t)b * p.max_pages) : nullptr;
+  const int64_t head_off = (int64_t)g * P * D;
+  const int64_t page_stride = (int64_t)p.hkv * P * D;
+
+  // Lane addresses.  Scores: key 32 t + (lane & 31), chunk 2 kk + half.  V: lane group of 16 reads 4 keys
+  // by 16 dims, key 8 r + 4 half + (lane & 15) / 4 of the step's 16, dims 32 d + 16 ((lane >> 4) & 1) + ...
+  // Both are a lane's base with the chunk's higher bits exclusive-or'ed in (slot()).
+  // They are kept, and toggled between the two buffers once a step.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)s_kv;
+  uint32_t ka[8], va[8];
+  {
+    const int kbase = (lane & 31) * (D * 2) + slot(lane & 15, half) * 16;
+    const int vrow = 4 * half + ((lane & 15) >> 2);
+    const int vbase = vrow * (D * 2) + slot(vrow, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 +
+                      8 * (lane & 1);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) ka[kk] = lds0 + (kbase ^ (32 * kk));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        va[2 * d + r] = lds0 + kTileBytes + 8 * r * (D * 2) + (vbase ^ (64 * d + 32 * r));
+  }
+
+  // A step's 4 pages go straight to LDS, one per wavefront.  The lanes' places there are consecutive, so
+  // the swizzle is in the addresses that they read from.  A page past the last repeats it (its keys are
+  // masked); one outside the pool is read as page 0 and its scores become NaN.
+  const int at = (lane >> 4) * (D * 2) + ((lane & 15) ^ (4 * (lane >> 4))) * 16;
+  struct Pages {
+    int of[kPagesPerTile];
+  };
+  auto entries = [&](int kt) {           // of step kt, or of the last one
+    Pages e;
+#pragma unroll
+    for (int j = 0; j < kPagesPerTile; ++j) e.of[j] = min(kt * kPagesPerTile + j, pages - 1);
+    if (bt) {
+#pragma unroll
+      for (int j = 0; j < kPagesPerTile; ++j) e.of[j] = bt[e.of[j]];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPagesPerTile; ++j) e.of[j] += b * p.max_pages;
+    }
+    return e;
+  };
+  const uint32_t lds = lds0 + wave * (P * D * 2);
+  // This wavefront's page of a step; bit j of bad: page j is outside the pool.
+  auto my_page = [&](const Pages& e, int& bad) {
+    int mine = 0;
+    bad = 0;
+#pragma unroll
+    for (int j = 0; j < kPagesPerTile; ++j) {
+      const bool in = (unsigned)e.of[j] < (unsigned)p.num_pages;
+      bad |= in ? 0 : 1 << j;
+      if (j == wave) mine = in ? e.of[j] : 0;
+    }
+    return mine;
+  };
+  auto load_k = [&](int page, int to) { load_page(p.k + page * page_stride + head_off, at, lds + to); };
+  auto load_v = [&](int page, int to) {
+    load_page(p.v + page * page_stride + head_off, at, lds + to + kTileBytes);
+  };
+
+  // From step `edge` on, some row of the tile does not see every key.  A masked key's weight is 0, but 0
+  // times an infinity or NaN is not: so every wavefront makes zeros of those in its page of V.  Where there
+  // were any (rare), they are added at the end to the rows that do see them.
+  const int edge = max(k0, sees_of(seq, p.causal, work.first >> gshift) / kKeyTile);
+  auto clean = [&](int buffer) {
+    unsigned char* const mine = s_kv + buffer + kTileBytes + wave * (P * D * 2);
+    u32x4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = reinterpret_cast<const u32x4*>(mine)[64 * j + lane];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x4 y = {finite_pair(x[j].x), finite_pair(x[j].y), finite_pair(x[j].z), finite_pair(x[j].w)};
+      if (((x[j].x ^ y.x) | (x[j].y ^ y.y) | (x[j].z ^ y.z) | (x[j].w ^ y.w)) != 0) {
+        reinterpret_cast<u32x4*>(mine)[64 * j + lane] = y;
+        s_found = 1;
+      }
+    }
+    __syncthreads();
+  };
+
+  // A fragment of K or V for one matrix instruction: of K (i < 8) the unit's 32 keys by dims 16 i .. + 15, of V
+  // 16 keys by 32 dims.
+  auto fragment = [&](int unit, int i) __attribute__((always_inline)) -> bf16x8 {
+    if (i < 8)
+      return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(ka[i] + unit * kUnitBytes);
+    const int d = i & 3, u = (i - 8) >> 2;
+    s16x4 a[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      a[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(
+          va[2 * d + r] + unit * kUnitBytes + 16 * u * (D * 2)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // The highest of a unit's scores that the row sees.
+  auto highest = [&](const f32x16& n) __attribute__((always_inline)) {
+    float top = n[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, n[i]);
+    return top;
+  };
+  // Scores n, from position key0 on, are next to be weighed, their highest being `top`: where some are masked
+  // or in a bad page they are made so first, and where one is far above the reference, that is raised and
+  // what was summed at the old one, weights w whose product is still to come among it, scaled.
+  auto take = [&](f32x16& n, float top, u32x4 (&w)[2], int key0, int bad) __attribute__((always_inline)) {
+    if (key0 + kUnit > all_see || bad != 0) {
+      asm volatile("");                  // a branch, not 64 selections
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if ((bad >> (i / 8)) & 1) n[i] = NAN;
+        if (key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) n[i] = -INFINITY;
+      }
+      top = highest(n);
+    }
+    top = fmaxf(top, other_half(top));
+    if (!__any(fmaf(top, scale, -less) > kLazy) && !far) return;
+    // The reference moves by whole numbers, so the factor is a power of two and exact in bf16 too.
+    const float c_top = top * scale;
+    const bool up = is_far ? (top - m) * scale > kLazy : c_top - less > kLazy;
+    const bool now_far = up ? !(fabsf(c_top) <= kFar) : is_far;
+    const float raised = up && !now_far ? ceilf(c_top) : less;
+    const float f = !up ? 1.0f
+                        : exp2f(is_far ? (m - top) * scale : less - (now_far ? c_top : raised));
+    if (up) m = top;
+    is_far = now_far;
+    less = is_far ? 0.0f : raised;
+    far = __any(is_far);
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x2 both = {(__bf16)(mrg::bf16_lo(w[u][i]) * f), (__bf16)(mrg::bf16_hi(w[u][i]) * f)};
+        w[u][i] = __builtin_bit_cast(uint32_t, both);
+      }
+    if (is_far) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) n[i] -= m;
+    }
+  };
+  // Weights i and i + 1 of scores s, computed here and not where they are used next (they are kept as 8
+  // registers, not the 16 that they are rounded from, and between the matrix instructions).
+  auto weigh = [&](const f32x16& s, int i, u32x4 (&w)[2]) __attribute__((always_inline)) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -less));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], scale, -less));
+    const bf16x2 both = {(__bf16)e0, (__bf16)e1};
+    uint32_t bits = __builtin_bit_cast(uint32_t, both);
+    l += e0;
+    l += e1;
+    asm volatile("" : "+v"(bits), "+v"(l));
+    w[i / 8][i % 8 / 2] = bits;
+  };
+  auto score_part = [&](const bf16x8& a, int i, f32x16& n) __attribute__((always_inline)) {
+    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], n, 0, 0, 0);
+  };
+  auto product_part = [&](const bf16x8& a, int i, const u32x4 (&w)[2]) __attribute__((always_inline)) {
+    o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        a, __builtin_bit_cast(bf16x8, w[(i - 8) >> 2]), o[i & 3], 0, 0, 0);
+  };
+  // Unit `unit` of a step: the scores of the next step's unit (K at ka), the weights of the scores s, and the
+  // product of the older weights w (V at va), none of which waits for another: 16 matrix instructions with
+  // the vector instructions of one weight each between them, and the LDS reads kRing - 1 ahead.
+  auto pipeline = [&](int unit, bf16x8 (&ring)[kRing], const f32x16& s, const u32x4 (&w)[2],
+                      u32x4 (&now)[2], f32x16& n) __attribute__((always_inline)) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int ahead = 16 * unit + i + kRing - 1;
+      if (ahead < 32) ring[(i + kRing - 1) % kRing] = fragment(ahead / 16, ahead % 16);
+      if (i < 8)
+        score_part(ring[i % kRing], i, n);
+      else
+        product_part(ring[i % kRing], i, w);
+      if (i % 2 == 0) weigh(s, i, now);
+      if (i == 10) top = fmaxf(n[0], n[1]);
+      if (i >= 10 && i < 15)
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (2 + 3 * (i - 10) + j < 16) top = fmaxf(top, n[2 + 3 * (i - 10) + j]);
+      if (i == 14) asm volatile("" : "+v"(top));     // here, not behind the branches
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return top;
+  };
+
+  if (k0 < k1) {
+    // K runs a step ahead of V: the wait for step kt is for K of kt + 1 and V of kt, and behind it K of
+    // kt + 2 and V of kt + 1 are requested.
+    int bad0 = 0, bad1 = 0, bad2 = 0;                // of steps kt, kt + 1, kt + 2
+    int kt = k0, to = 0;                             // to: the buffer of kt
+    int page = my_page(entries(kt), bad0);           // this wavefront's, of the K requested last
+    load_k(page, 0);
+    load_v(page, 0);
+    if (kt + 1 < k1) {
+      page = my_page(entries(kt + 1), bad1);
+      load_k(page, kBufferBytes);
+    }
+    Pages next = entries(kt + 2);
+    if (threadIdx.x == 0) s_found = 0;
+    arrived();
+    f32x16 s, n;
+    u32x4 w[2] = {}, now[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = n[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) score_part(fragment(0, i), i, s);
+    take(s, highest(s), w, kt * kKeyTile, bad0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) score_part(fragment(1, i), i, n);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) weigh(s, i, w);
+    take(n, highest(n), w, kt * kKeyTile + kUnit, bad0 >> 2);
+    s = n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ka[i] ^= kBufferBytes;
+    for (; kt + 1 < k1; ++kt) {
+      arrived();                                     // K of kt + 1 and V of kt; older units are read
+      load_v(page, to ^ kBufferBytes);
+      bad2 = 0;
+      if (kt + 2 < k1) {
+        page = my_page(next, bad2);
+        load_k(page, to);
+        next = entries(kt + 3);
+      }
+      if (kt >= edge) clean(to);
+      bf16x8 ring[kRing];
+#pragma unroll
+      for (int i = 0; i < kRing - 1; ++i) ring[i] = fragment(0, i);
+      float top = pipeline(0, ring, s, w, now, n);
+      take(n, top, now, (kt + 1) * kKeyTile, bad1);
+      top = pipeline(1, ring, n, now, w, s);
+      take(s, top, w, (kt + 1) * kKeyTile + kUnit, bad1 >> 2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ka[i] ^= kBufferBytes;
+        va[i] ^= kBufferBytes;
+      }
+      bad1 = bad2;
+      to ^= kBufferBytes;
+    }
+    arrived();
+    if (kt >= edge) clean(to);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) weigh(s, i, now);
+#pragma unroll
+    for (int i = 8; i < 16; ++i) product_part(fragment(0, i), i, w);
+#pragma unroll
+    for (int i = 8; i < 16; ++i) product_part(fragment(1, i), i, now);
+
+    if (s_found != 0) {                              // infinities and NaN among the keys from `edge` on
+#pragma unroll 1
+      for (int pos = edge * kKeyTile; pos < min(keys, k1 * kKeyTile); ++pos) {
+        const int entry = bt ? bt[pos / P] : b * p.max_pages + pos / P;
+        if ((unsigned)entry >= (unsigned)p.num_pages) continue;    // its scores are NaN
+        const uint16_t* const x = p.v + entry * page_stride + head_off + (pos % P) * D + 4 * half;
+        if (pos >= sees) continue;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t v = x[32 * d + 8 * (i / 4) + i % 4];
+            if ((v & 0x7f80u) == 0x7f80u) o[d][i] += mrg::bf16_lo(v);
+          }
+      }
+    }
+  }
+
+  l += other_half(l);
+  const bool empty = l == 0.0f;          // no position, or every score -inf
+  const float inv = poison ? NAN : empty ? 0.0f : 1.0f / l;
+  const float lse = poison ? NAN : empty ? -INFINITY : ((is_far ? m * scale : less) + log2f(l)) * kLn2;
+  const bool to_pairs = parts > 1 || p.out == nullptr;
+  if (live && half == 0) {
+    if (to_pairs)
+      p.part_lse[(out_row * p.entries + work.part) * p.hq + h] = lse;
+    else if (p.lse != nullptr)
+      p.lse[out_row * p.hq + h] = lse;
+  }
+  // A lane has 4 neighbouring dims of a row at a time; through LDS (the buffer that the last step is not
+  // in, 8 KB a wavefront, swizzled as a page is) 16 lanes store 256 bytes of one.
+  unsigned char* const swap =
+      s_kv + (((k1 - k0) & 1) != 0 ? kBufferBytes : 0) + wave * (kRowsPerWave * D * 2);
+  const int c = lane & 15;
+  auto store = [&](auto to) {            // row 4 j + lane / 16 of the wavefront, to(its place, its chunk c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 4 * j + (lane >> 4), at_row = work.first + wave * kRowsPerWave + r;
+      const u32x4 x = *reinterpret_cast<const u32x4*>(swap + r * (D * 2) + (c ^ (r & 15)) * 16);
+      const int64_t token = seq.start + (at_row >> gshift);
+      if (at_row < n_rows) *to(token, (g << gshift) + (at_row & ((1 << gshift) - 1))) = x;
+    }
+  };
+  const int mine = lane & 31;
+  if (to_pairs) {
+#pragma unroll
+    for (int q2 = 0; q2 < 2; ++q2) {     // 64 dims at a time
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const f32x16& x = o[2 * q2 + d];
+          *reinterpret_cast<float4*>(swap + mine * (D * 2) + ((8 * d + 2 * a + half) ^ (mine & 15)) * 16) =
+              make_float4(x[4 * a] * inv, x[4 * a + 1] * inv, x[4 * a + 2] * inv, x[4 * a + 3] * inv);
+        }
+      store([&](int64_t token, int head) {
+        return reinterpret_cast<u32x4*>(p.part_o + ((token * p.entries + work.part) * p.hq + head) * D) +
+               16 * q2 + c;
+      });
+    }
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = empty && !poison ? 0.0f : o[d][4 * a + j] * inv;
+        const bf16x2 lo = {(__bf16)x[0], (__bf16)x[1]}, hi = {(__bf16)x[2], (__bf16)x[3]};
+        *reinterpret_cast<uint2*>(swap + mine * (D * 2) + ((4 * d + a) ^ (mine & 15)) * 16 + 8 * half) =
+            make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+      }
+    store([&](int64_t token, int head) {
+      return reinterpret_cast<u32x4*>(p.out + (token * p.hq + head) * D) + c;
+    });
+  }
+}
+
+}  // namespace rows
+}  // namespace qf
