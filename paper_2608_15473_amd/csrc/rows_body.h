@@ -510,17 +510,41 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
       for (int i = 0; i < 16; ++i) n[i] -= m;
     }
   };
-  // Weights i and i + 1 of scores s, computed here and not where they are used next (they are kept as 8
-  // registers, not the 16 that they are rounded from, and between the matrix instructions).
-  auto weigh = [&](const f32x16& s, int i, u32x4 (&w)[2]) __attribute__((always_inline)) {
-    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -less));
-    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], scale, -less));
-    const bf16x2 both = {(__bf16)e0, (__bf16)e1};
-    uint32_t bits = __builtin_bit_cast(uint32_t, both);
-    l += e0;
-    l += e1;
-    asm volatile("" : "+v"(bits), "+v"(l));
-    w[i / 8][i % 8 / 2] = bits;
+  // The weights of a unit in three stages of one vector instruction each: the exponent, the power, and its
+  // place in the sum and (with the one before it) in a bf16 pair.  stage(i) is the third of weight i, the
+  // second of i + 1 and the first of i + 2: none waits for another.  Pinned: the compiler would move them to
+  // where the pairs are used, with twice the registers and away from the matrix instructions.
+  float exponent[2], power[2], even = 0.0f;
+  auto first_stage = [&](const f32x16& s, int i) __attribute__((always_inline)) {
+    if (i < 16) exponent[i % 2] = fmaf(s[i], scale, -less);
+  };
+  auto second_stage = [&](int i) __attribute__((always_inline)) {
+    if (i < 16) power[i % 2] = __builtin_amdgcn_exp2f(exponent[i % 2]);
+  };
+  auto begin_weights = [&](const f32x16& s) __attribute__((always_inline)) {
+    first_stage(s, 0);
+    first_stage(s, 1);
+    second_stage(0);
+  };
+  auto stage = [&](const f32x16& s, int i, u32x4 (&w)[2]) __attribute__((always_inline)) {
+    float e = power[i % 2];
+    second_stage(i + 1);
+    first_stage(s, i + 2);
+    l += e;
+    if (i % 2 == 0) {
+      asm volatile("" : "+v"(e), "+v"(l), "+v"(power[(i + 1) % 2]), "+v"(exponent[i % 2]));
+      even = e;
+    } else {
+      const bf16x2 both = {(__bf16)even, (__bf16)e};
+      uint32_t bits = __builtin_bit_cast(uint32_t, both);
+      asm volatile("" : "+v"(bits), "+v"(l), "+v"(power[(i + 1) % 2]), "+v"(exponent[i % 2]));
+      w[i / 8][i % 8 / 2] = bits;
+    }
+  };
+  auto weigh_all = [&](const f32x16& s, u32x4 (&w)[2]) __attribute__((always_inline)) {
+    begin_weights(s);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) stage(s, i, w);
   };
   auto score_part = [&](const bf16x8& a, int i, f32x16& n) __attribute__((always_inline)) {
     n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], n, 0, 0, 0);
@@ -537,6 +561,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+    begin_weights(s);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int ahead = 16 * unit + i + kRing - 1;
@@ -545,13 +570,12 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
         score_part(ring[i % kRing], i, n);
       else
         product_part(ring[i % kRing], i, w);
-      if (i % 2 == 0) weigh(s, i, now);
-      if (i == 10) top = fmaxf(n[0], n[1]);
-      if (i >= 10 && i < 15)
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-          if (2 + 3 * (i - 10) + j < 16) top = fmaxf(top, n[2 + 3 * (i - 10) + j]);
-      if (i == 14) asm volatile("" : "+v"(top));     // here, not behind the branches
+      stage(s, i, now);
+      // the highest score; n is complete after i = 7
+      if (i == 9) top = fmaxf(fmaxf(n[0], n[1]), n[2]);
+      if (i > 9) top = fmaxf(fmaxf(top, n[2 * i - 17]), n[2 * i - 16]);
+      if (i == 15) top = fmaxf(top, n[15]);
+      if (i >= 9) asm volatile("" : "+v"(top));      // here, not behind the branches
       __builtin_amdgcn_sched_barrier(0);
     }
     return top;
@@ -581,8 +605,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
     take(s, highest(s), w, kt * kKeyTile, bad0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) score_part(fragment(1, i), i, n);
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) weigh(s, i, w);
+    weigh_all(s, w);
     take(n, highest(n), w, kt * kKeyTile + kUnit, bad0 >> 2);
     s = n;
 #pragma unroll
@@ -614,8 +637,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
     }
     arrived();
     if (kt >= edge) clean(to);
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) weigh(s, i, now);
+    weigh_all(s, now);
 #pragma unroll
     for (int i = 8; i < 16; ++i) product_part(fragment(0, i), i, w);
 #pragma unroll
