@@ -171,6 +171,8 @@ struct RowsParams {
 };
 constexpr int kRowsTile = 128;  // query rows (tokens x query heads of a KV head) of a workgroup
 constexpr int kKeyTile = 64;    // positions of a step
+// What key ranges cost and save, us (rows_body.h: range_of).
+constexpr float kRowsAloneUs = 1.2f, kRowsStepUs = 2.0f, kRowsJoinUs = 8.0f, kRowsPairUs = 3.44e-4f;
 // Every sequence has at most one tile that is not full.
 inline int64_t rows_tiles(int64_t rows, int64_t group, int64_t seqs) {
   return rows * group / kRowsTile + (seqs < rows ? seqs : rows);

@@ -293,13 +293,18 @@ constexpr int64_t kPairBytes = 128 << 20;
 struct Items {
   int64_t slots = 0, entries = 1;
 };
-Items rows_items(int64_t rows, int64_t hq, int64_t hkv, int64_t seqs, int64_t max_pages) {
+// `direct`: a tile with one range writes its outputs itself; then a table too short for ranges ever to pay
+// (rows_body.h: range_of) takes none, and no join.
+Items rows_items(int64_t rows, int64_t hq, int64_t hkv, int64_t seqs, int64_t max_pages, bool direct) {
   const int64_t steps = (max_pages * qf::kPage + qf::kKeyTile - 1) / qf::kKeyTile;
   const int64_t full = rows * (hq / hkv) / qf::kRowsTile;
   const int64_t in_bytes = kPairBytes / (rows * hq * (qf::kHeadDim + 1) * (int64_t)sizeof(float));
   Items it;
   it.slots = qf::rows_tiles(rows, hq / hkv, seqs);
   if (it.slots >= kRowsResident / hkv) return it;
+  if (direct && qf::kRowsAloneUs * (float)steps <=
+                    qf::kRowsStepUs + qf::kRowsJoinUs + 0.5f * qf::kRowsPairUs * (float)(rows * hq))
+    return it;
   it.entries = std::max<int64_t>(1, std::min({kRowsResident / hkv - full + 1, steps, kMostEntries,
                                               std::max<int64_t>(4, in_bytes)}));
   if (it.entries > 1) it.slots = kRowsResident / hkv;
@@ -351,7 +356,8 @@ int plan_prefill(const qf_decode_desc* desc, int32_t n_tokens, Prefill* pl) {
     *pl = Prefill{};
     return QF_OK;
   }
-  pl->items = rows_items(n_tokens, desc->n_q_heads, desc->n_kv_heads, desc->batch, desc->max_pages_per_seq);
+  pl->items = rows_items(n_tokens, desc->n_q_heads, desc->n_kv_heads, desc->batch, desc->max_pages_per_seq,
+                         true);
   pl->bytes = pl->items.entries > 1
                   ? pair_floats(n_tokens, pl->items.entries, desc->n_q_heads) * sizeof(float) : 0;
   // The most workgroups of a launch, and the rows of the join.
@@ -380,7 +386,7 @@ int plan_shared(const qf_decode_desc* desc, int32_t n_groups, int32_t max_prefix
   pl->slots = d.max_shards * choose_chunks(&d);
   if (pl->slots > INT32_MAX) return fail(QF_EINVAL, "max_shards * chunks exceeds int32");
   if (n_groups > 0) {
-    pl->items = rows_items(d.batch, d.n_q_heads, d.n_kv_heads, n_groups, max_prefix_pages);
+    pl->items = rows_items(d.batch, d.n_q_heads, d.n_kv_heads, n_groups, max_prefix_pages, false);
     pl->prefix_floats = pair_floats(d.batch, pl->items.entries, d.n_q_heads);
     const int64_t units = (int64_t)d.batch * pl->slots * d.n_kv_heads;
     if (pl->items.slots * d.n_kv_heads + units + units / 8 + 64 > kMaxGrid)

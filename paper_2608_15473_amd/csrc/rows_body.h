@@ -50,11 +50,27 @@ constexpr int kRing = 4;                             // fragments in registers
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;            // log2 units: p <= 256 between rescales
 constexpr float kFar = 1048576.0f;       // log2 units
-// The shortest range: one step per 32 rows of the fullest tile.  A row's pair is 516 bytes written and read
-// again, a step 32 KB, so full tiles would move more bytes for their pairs than for their keys below 4
-// steps (32 requests over 8,192 positions, G = 4: 14.6 us with 4, 16.6 with 3), few rows take the latency
-// of a range instead (4 requests over 1,531 positions, G = 2: 10.9 us with 4 steps, 7.3 with 1).
-__device__ __forceinline__ int least_range(int rows) { return (min(rows, kRowsTile) + 31) / 32; }
+// Steps of a key range, from what is known of all tiles of a KV head: `all` steps of `tiles` tiles, the longest
+// of `longest`.  The least that fits the items and the entries fills the chip, but ranges cost too: a row's
+// pair is 516 bytes written and read again, kRowsPairUs a range of all rows and heads, so a range is at least
+// as long as minimises kRowsStepUs range + pair avg / range; and where no cut at all is faster, there is none:
+//   uncut          kRowsAloneUs (with a workgroup to a compute unit, else kRowsStepUs) x longest
+//   ranges         kRowsStepUs x range + kRowsJoinUs + pair (avg / range + 1/2)
+// Measured (us, cut to fill the chip / uncut): 1,024 causal tokens at 16/8 heads 32.8 / 24.2, 2,048 54.7 /
+// 44.1, 128 11.4 / 8.4, but 256 tokens after 4,096 32.2 / 81; 32 rows over 8,192 positions at 32/8 heads
+// 14.6 with 4 steps a range, 16.6 with 3.
+__device__ __forceinline__ int range_of(const RowsParams& p, int64_t all, int64_t tiles, int longest) {
+  if (tiles == 0) return 1;
+  const int64_t room = p.slots - tiles;
+  int64_t least = room > 0 ? (all + room - 1) / room : INT32_MAX;
+  least = max(least, (int64_t)((longest + p.entries - 1) / p.entries));
+  const float avg = (float)all / (float)tiles, pair = kRowsPairUs * (float)p.rows * (float)p.hq;
+  const int64_t range = max(least, (int64_t)ceilf(sqrtf(pair * avg / kRowsStepUs)));
+  const float uncut = (tiles * p.hkv <= 256 ? kRowsAloneUs : kRowsStepUs) * (float)longest;
+  const float cut = kRowsStepUs * (float)range + kRowsJoinUs + pair * (avg / (float)range + 0.5f);
+  if (p.out != nullptr && uncut <= cut) return INT32_MAX;
+  return (int)min(max(range, (int64_t)1), (int64_t)INT32_MAX);
+}
 static_assert(kPagesPerTile == W, "a wavefront stages one page of each step");
 
 typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
@@ -213,8 +229,8 @@ __device__ __forceinline__ Work longest_first(const RowsParams& p, int gshift, i
 }
 
 // Work item `slot` of a KV head; every wavefront finds it for itself, lane l looking at sequences l, l + 64, ...
-// The range is the least that leaves at most p.slots items and p.entries ranges a tile: with t tiles of n
-// steps each sequence has t ceil(n / range) of them.  Items of a range of keys lie side by side (their
+// The range (range_of) leaves at most p.slots items and p.entries ranges a tile: with t tiles of n steps each
+// sequence has t ceil(n / range) of them.  Items of a range of keys lie side by side (their
 // tiles read the same keys).  Causal tiles without ranges differ in length: longest_first.
 __device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int slot) {
   const int lane = threadIdx.x & 63;
@@ -224,12 +240,7 @@ __device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int s
                                 p.rows, p.max_pages, p.causal, 0);
     const int t = tiles_of(q, gshift);
     const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
-    if (p.entries > 1) {
-      const int64_t room = p.slots - t;
-      const int64_t r = room > 0 ? ((int64_t)t * n + room - 1) / room : INT32_MAX;
-      range = (int)min(max(max(r, (int64_t)((n + p.entries - 1) / p.entries)),
-                           (int64_t)least_range(q.len << gshift)), (int64_t)INT32_MAX);
-    }
+    if (p.entries > 1) range = __builtin_amdgcn_readfirstlane(range_of(p, (int64_t)t * n, t, n));
     const int parts = ranges_of(n, range);
     if (slot >= t * parts) return Work{-1, 0, 0, range, q};
     const int i = p.entries > 1 ? slot : t - 1 - slot;
@@ -237,7 +248,7 @@ __device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int s
   }
   if (p.entries > 1) {
     int64_t all = 0, tiles = 0;
-    int longest = 0, most = 0;
+    int longest = 0;
     for (int b0 = 0; b0 < p.seqs; b0 += 64) {
       const int b = b0 + lane;
       if (b < p.seqs) {
@@ -247,17 +258,12 @@ __device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int s
         all += (int64_t)t * n;
         tiles += t;
         longest = max(longest, n);
-        most = max(most, q.len << gshift);
       }
     }
     all = wave_sum(all);
     tiles = wave_sum(tiles);
     longest = wave_max(longest);
-    most = wave_max(most);
-    const int64_t room = p.slots - tiles;
-    int64_t r = room > 0 ? (all + room - 1) / room : INT32_MAX;
-    r = max(r, (int64_t)((longest + p.entries - 1) / p.entries));
-    range = __builtin_amdgcn_readfirstlane((int)min(max(r, (int64_t)least_range(most)), (int64_t)INT32_MAX));
+    range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
   } else if (p.causal) {
     return longest_first(p, gshift, slot);
   }

@@ -245,6 +245,13 @@ PREFILL = [
 ]
 
 
+PREFILL += [
+    dict(hq=4, hkv=2, lens=[3, 0, 40], ctx=[2, 0, 6000], sharp=2.0),     # one tile cut, others not
+    dict(hq=1, hkv=1, lens=[1 + b % 2 for b in range(100)], ctx=[3000 if b == 77 else b for b in range(100)]),
+    dict(hq=32, hkv=4, lens=[33], ctx=[2500], sharp=2.0),                # full tiles, cut
+]
+
+
 @pytest.mark.parametrize("kw", PREFILL, ids=range(len(PREFILL)))
 def test_prefill(gpu, kw):
     c = prefill_case(21, **kw)
@@ -436,6 +443,13 @@ SHARED = [
     dict(hq=8, hkv=2, rows=[0, 2, 5], prefix=[0, 16], ctx=[0, 3, 0, 40, 1], shards=1),
     dict(hq=2, hkv=2, rows=[0, 2], prefix=[9001], ctx=[11, 2000], shards=7),
     dict(hq=2, hkv=1, rows=[2, 2], prefix=[64], ctx=[5, 0, 33]),               # nobody shares it
+]
+
+
+SHARED += [
+    dict(hq=2, hkv=1, rows=[*range(71)], prefix=[1500 if i == 66 else 5 * i for i in range(70)],
+         ctx=[b % 9 for b in range(71)], shards=1),
+    dict(hq=16, hkv=2, rows=[0, 20, 90], prefix=[3000, 700], ctx=[7 * b % 41 for b in range(90)], sharp=2.0),
 ]
 
 
