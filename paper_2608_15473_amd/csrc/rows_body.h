@@ -112,12 +112,12 @@ __device__ __forceinline__ void arrived() {
 // Sequence b: its rows (none where they are out of order or range) and the positions before them.
 struct Sequence {
   int start, len, before;
-  bool poison;                           // a length out of range: no position is read
+  int poison;                            // a length out of range: no position is read
 };
 __device__ __forceinline__ Sequence sequence(const int32_t* __restrict__ cu,
                                              const int32_t* __restrict__ ctx_lens, int32_t rows,
                                              int32_t max_pages, bool causal, int b) {
-  Sequence q{0, 0, 0, false};
+  Sequence q{0, 0, 0, 0};
   const int s = cu[b], e = cu[b + 1], n = ctx_lens[b];
   if (s < 0 || e <= s || e > rows) return q;
   q.start = s;
@@ -141,15 +141,17 @@ __device__ __forceinline__ int tiles_of(const Sequence& q, int gshift) {
 // A tile's keys are cut into ranges of `range` steps.
 __device__ __forceinline__ int ranges_of(int steps, int range) { return steps > 0 ? (steps - 1) / range + 1 : 1; }
 
+// Sum and maximum over the lanes, in scalar registers.
 __device__ __forceinline__ int64_t wave_sum(int64_t x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  const uint32_t high = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)((uint64_t)high << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return x;
+  return __builtin_amdgcn_readfirstlane(x);
 }
 
 // What a workgroup does: rows first .. first + 127 of sequence seq, key range `part`.
@@ -161,139 +163,177 @@ struct Work {
 // (n - 1) kKeyTile positions.
 __device__ __forceinline__ int tiles_from(const Sequence& q, int gshift, int tiles, int n) {
   if (q.poison) return n <= 0 ? tiles : 0;
-  const int need = max(0, (n - 1) * kKeyTile - q.before);        // rows before the first such row
+  const int64_t need = max((int64_t)0, (int64_t)(n - 1) * kKeyTile - q.before);   // rows before the first such
   if (need >= q.len) return 0;
-  return tiles - (int)(((int64_t)need << gshift) / kRowsTile);
+  return tiles - (int)((need << gshift) / kRowsTile);
 }
-// The slot-th tile in order of length, the longest first, of causal sequences (a workgroup that starts late
-// has to be short): by bisection for its number of steps, then among the tiles of just that many.
-__device__ __forceinline__ Work longest_first(const RowsParams& p, int gshift, int slot) {
-  const int lane = threadIdx.x & 63;
-  auto each = [&](auto use) {            // every sequence, 64 at a time, one per lane
-    for (int b0 = 0; b0 < p.seqs; b0 += 64) {
-      Sequence q{0, 0, 0, false};
-      if (b0 + lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, true, b0 + lane);
-      if (use(b0, q)) return;
-    }
-  };
-  auto count = [&](int n) {              // tiles of at least n steps
-    int64_t sum = 0;
-    each([&](int, const Sequence& q) {
-      sum += tiles_from(q, gshift, tiles_of(q, gshift), n);
-      return false;
-    });
-    return wave_sum(sum);
-  };
-  int low = 0, high = (int)min((int64_t)p.max_pages * P / kKeyTile + 2, (int64_t)INT32_MAX);
-  if (p.seqs <= 64) {                    // the usual case: one sequence per lane, read once
-    Sequence q{0, 0, 0, false};
-    if (lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, true, lane);
-    const int t = tiles_of(q, gshift);
-    high = wave_max(t > 0 ? steps_of(sees_of(q, true, q.len - 1)) + 1 : 1);
-    while (high - low > 1) {             // count(low) > slot >= count(high), if slot has a tile at all
-      const int n = (low + high) / 2;
-      if (wave_sum((int64_t)tiles_from(q, gshift, t, n)) > slot) low = n; else high = n;
-    }
-  } else {
-    while (high - low > 1) {
-      const int n = (low + high) / 2;
-      if (count(n) > slot) low = n; else high = n;
-    }
-  }
-  int64_t before = count(low + 1);
-  Work w{-1, 0, 0, INT32_MAX, Sequence{0, 0, 0, false}};
-  each([&](int b0, const Sequence& q) {
-    const int t = tiles_of(q, gshift);
-    const int above = tiles_from(q, gshift, t, low + 1);
-    const int64_t items = tiles_from(q, gshift, t, low) - above;
-    int64_t upto = items;
+// Running sum over the lanes, this one's included.
+__device__ __forceinline__ int64_t upto_sum(int64_t x) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
-    const uint64_t past = __ballot(before + upto > slot);
-    if (past == 0) {
-      before += __shfl(upto, 63);
-      return false;
-    }
-    const int l = __builtin_ctzll(past);
-    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-    const int i = __builtin_amdgcn_readfirstlane(slot - (int)(before + __shfl(upto - items, l)));
-    w.seq = b0 + l;
-    w.first = (of(t) - of(above) - 1 - i) * kRowsTile;
-    w.q = Sequence{of(q.start), of(q.len), of(q.before), of(q.poison) != 0};
-    return true;
-  });
-  return w;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if ((int)(threadIdx.x & 63) >= o) x += y;
+  }
+  return x;
 }
 
-// Work item `slot` of a KV head; every wavefront finds it for itself, lane l looking at sequences l, l + 64, ...
-// The range (range_of) leaves at most p.slots items and p.entries ranges a tile: with t tiles of n steps each
-// sequence has t ceil(n / range) of them.  Items of a range of keys lie side by side (their
-// tiles read the same keys).  Causal tiles without ranges differ in length: longest_first.
-__device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int slot) {
+// Work item `slot` of a KV head.  The range (range_of) leaves at most p.slots items and p.entries ranges a
+// tile: with t tiles of n steps each sequence has t ceil(n / range) of them.  Items of a range of keys lie
+// side by side (their tiles read the same keys).  Causal tiles without ranges differ in length: they are taken
+// the longest first (a workgroup that starts late has to be short), by bisection for the slot-th tile's number
+// of steps, then among the tiles of just that many.
+// At most 64 sequences: every wavefront finds it for itself, a lane to a sequence.
+__device__ __forceinline__ Work find_among_few(const RowsParams& p, int gshift, int slot) {
   const int lane = threadIdx.x & 63;
-  int range = INT32_MAX;
-  if (p.seqs == 1) {                     // by scalar instructions alone
-    const Sequence q = sequence((const int32_t*)(const_i32_ptr)p.cu, (const int32_t*)(const_i32_ptr)p.ctx_lens,
-                                p.rows, p.max_pages, p.causal, 0);
-    const int t = tiles_of(q, gshift);
-    const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
-    if (p.entries > 1) range = __builtin_amdgcn_readfirstlane(range_of(p, (int64_t)t * n, t, n));
-    const int parts = ranges_of(n, range);
-    if (slot >= t * parts) return Work{-1, 0, 0, range, q};
-    const int i = p.entries > 1 ? slot : t - 1 - slot;
-    return Work{0, i % t * kRowsTile, i / t, range, q};
+  Sequence q{0, 0, 0, 0};
+  if (lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, lane);
+  const int t = tiles_of(q, gshift);
+  const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
+  const bool by_length = p.entries == 1 && p.causal;
+  int range = INT32_MAX, above = 0;      // above: tiles of the sequence that are longer
+  int64_t before = 0, items;
+  if (by_length) {
+    int low = 0, high = wave_max(n) + 1; // tiles of at least low, high steps: > slot (or none), <= slot
+    while (high - low > 1) {
+      const int mid = (low + high) / 2;
+      if (wave_sum((int64_t)tiles_from(q, gshift, t, mid)) > slot) low = mid; else high = mid;
+    }
+    above = tiles_from(q, gshift, t, low + 1);
+    before = wave_sum(above);
+    items = tiles_from(q, gshift, t, low) - above;
+  } else {
+    if (p.entries > 1) {
+      const int64_t all = wave_sum((int64_t)t * n), tiles = wave_sum(t);
+      const int longest = wave_max(n);
+      range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
+    }
+    items = (int64_t)t * ranges_of(n, range);
   }
-  if (p.entries > 1) {
+  const int64_t upto = before + upto_sum(items);
+  const uint64_t past = __ballot(upto > slot);
+  if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
+  const int l = __builtin_ctzll(past);
+  auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+  const int i = __builtin_amdgcn_readfirstlane(slot - (int)__shfl(upto - items, l)), tl = of(t);
+  const Sequence found{of(q.start), of(q.len), of(q.before), of(q.poison)};
+  if (by_length) return Work{l, (tl - of(above) - 1 - i) * kRowsTile, 0, range, found};
+  return Work{l, i % tl * kRowsTile, i / tl, range, found};
+}
+
+// More sequences: the workgroup together, thread t looking at sequences t, t + 256, ...; their items lie in
+// order of (t, sequence).  Tiles of different lengths go by their number of bits of steps, the most first,
+// counted in one pass.
+struct Many {
+  int64_t all[W], tiles[W];              // sums of each wavefront
+  int longest[W];
+  int tiles_of_bits[33];
+  Work work;
+};
+__device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift, int slot, Many& lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool by_length = p.entries == 1 && p.causal;
+  int range = INT32_MAX, bits = 0;
+  int64_t before = 0;
+  auto each = [&](auto use) {            // this thread's sequences: their tiles, and steps of the longest
+    for (int b = threadIdx.x; b < p.seqs; b += 64 * W) {
+      const Sequence q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, b);
+      const int t = tiles_of(q, gshift);
+      use(b, q, t, t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0);
+    }
+  };
+  // Tiles whose number of steps has at least k bits.
+  auto with_bits = [&](const Sequence& q, int t, int k) {
+    return k > 31 ? 0 : tiles_from(q, gshift, t, k == 0 ? 0 : 1 << (k - 1));
+  };
+  if (threadIdx.x == 0) lds.work = Work{-1, 0, 0, 0, Sequence{0, 0, 0, 0}};
+  if (by_length) {
+    if (threadIdx.x < 33) lds.tiles_of_bits[threadIdx.x] = 0;
+    __syncthreads();
+    each([&](int, const Sequence& q, int t, int n) {
+      int longer = 0;
+      for (int k = n > 0 ? 32 - __builtin_clz(n) : 0; longer < t && k >= 0; --k) {
+        const int so_far = with_bits(q, t, k);
+        if (so_far > longer) atomicAdd(&lds.tiles_of_bits[k], so_far - longer);
+        longer = so_far;
+      }
+    });
+    __syncthreads();
+    const int64_t items = lane < 33 ? lds.tiles_of_bits[32 - lane] : 0;
+    const int64_t upto = upto_sum(items);
+    const uint64_t past = __ballot(upto > slot);
+    if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
+    const int l = __builtin_ctzll(past);
+    bits = __builtin_amdgcn_readfirstlane(32 - l);
+    before = __shfl(upto - items, l);
+  } else if (p.entries > 1) {
     int64_t all = 0, tiles = 0;
     int longest = 0;
-    for (int b0 = 0; b0 < p.seqs; b0 += 64) {
-      const int b = b0 + lane;
-      if (b < p.seqs) {
-        const Sequence q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, b);
-        const int t = tiles_of(q, gshift);
-        const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
-        all += (int64_t)t * n;
-        tiles += t;
-        longest = max(longest, n);
-      }
-    }
+    each([&](int, const Sequence&, int t, int n) {
+      all += (int64_t)t * n;
+      tiles += t;
+      longest = max(longest, n);
+    });
     all = wave_sum(all);
     tiles = wave_sum(tiles);
     longest = wave_max(longest);
+    if (lane == 0) {
+      lds.all[wave] = all;
+      lds.tiles[wave] = tiles;
+      lds.longest[wave] = longest;
+    }
+    __syncthreads();
+    all = tiles = longest = 0;
+    for (int w = 0; w < W; ++w) {
+      all += lds.all[w];
+      tiles += lds.tiles[w];
+      longest = max(longest, lds.longest[w]);
+    }
     range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
-  } else if (p.causal) {
-    return longest_first(p, gshift, slot);
   }
-  int64_t before = 0;                    // items of the sequences before this round's
-  for (int b0 = 0; b0 < p.seqs; b0 += 64) {
-    const int b = b0 + lane;
-    Sequence q{0, 0, 0, false};
-    if (b < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, b);
-    const int t = tiles_of(q, gshift);
-    const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
-    const int64_t items = (int64_t)t * ranges_of(n, range);
-    int64_t upto = items;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
-    const uint64_t past = __ballot(before + upto > slot);
-    if (past != 0) {
-      const int l = __builtin_ctzll(past);
-      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-      const int i = slot - (int)(before + __shfl(upto - items, l));
-      const int tl = of(t);
-      const int il = __builtin_amdgcn_readfirstlane(i);
-      return Work{b0 + l, il % tl * kRowsTile, il / tl, range,
-                  Sequence{of(q.start), of(q.len), of(q.before), of(q.poison) != 0}};
-    }
-    before += __shfl(upto, 63);
-  }
-  return Work{-1, 0, 0, range, Sequence{0, 0, 0, false}};
+  auto items_of = [&](const Sequence& q, int t, int n) {
+    return by_length ? (int64_t)(with_bits(q, t, bits) - with_bits(q, t, bits + 1))
+                     : (int64_t)t * ranges_of(n, range);
+  };
+  int64_t mine = 0;
+  each([&](int, const Sequence& q, int t, int n) { mine += items_of(q, t, n); });
+  int64_t upto = upto_sum(mine);
+  __syncthreads();                       // the sums above are read
+  if (lane == 63) lds.all[wave] = upto;
+  __syncthreads();
+  upto += before;
+  for (int w = 0; w < wave; ++w) upto += lds.all[w];
+  int64_t at = slot - (upto - mine);     // among this thread's, in one thread of the workgroup
+  if (at >= 0 && at < mine)
+    each([&](int b, const Sequence& q, int t, int n) {
+      const int64_t items = items_of(q, t, n);
+      if (at >= 0 && at < items) {
+        const int i = (int)at;
+        lds.work = by_length ? Work{b, (t - with_bits(q, t, bits + 1) - 1 - i) * kRowsTile, 0, range, q}
+                             : Work{b, i % t * kRowsTile, i / t, range, q};
+      }
+      at -= items;
+    });
+  __syncthreads();
+  Work found = lds.work;
+  found.range = range;
+  __syncthreads();                       // read, before the keys take its place
+  return found;
+}
+
+__device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int slot, Many& lds) {
+  if (p.seqs > 64) return find_among_many(p, gshift, slot, lds);
+  if (p.seqs > 1) return find_among_few(p, gshift, slot);
+  // One: by scalar instructions alone; causal tiles grow longer with their number.
+  const Sequence q = sequence((const int32_t*)(const_i32_ptr)p.cu, (const int32_t*)(const_i32_ptr)p.ctx_lens,
+                              p.rows, p.max_pages, p.causal, 0);
+  const int t = tiles_of(q, gshift);
+  const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
+  int range = INT32_MAX;
+  if (p.entries > 1) range = __builtin_amdgcn_readfirstlane(range_of(p, (int64_t)t * n, t, n));
+  const int parts = ranges_of(n, range);
+  if (slot >= t * parts) return Work{-1, 0, 0, range, q};
+  const int i = p.entries > 1 ? slot : t - 1 - slot;
+  return Work{0, i % t * kRowsTile, i / t, range, q};
 }
 
 // A bf16 pair with zeros for infinities and NaN.
@@ -303,9 +343,13 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
   return w;
 }
 
-// A workgroup's LDS: two steps' K and V, and whether V had infinities or NaN among masked steps.
+// A workgroup's LDS: two steps' K and V (before them, what finds the work item), and whether V had infinities
+// or NaN among masked steps.
 struct Lds {
-  alignas(1024) unsigned char kv[2 * kBufferBytes];
+  union {
+    alignas(1024) unsigned char kv[2 * kBufferBytes];
+    Many many;
+  };
   int found;
 };
 
@@ -319,7 +363,10 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
   const int gshift = 31 - __builtin_clz(p.hq / p.hkv);
 
   const int g = item % (unsigned)p.hkv;
-  const Work work = find_work(p, gshift, item / (unsigned)p.hkv);
+  Work work = find_work(p, gshift, item / (unsigned)p.hkv, lds_mem.many);
+  for (int* x : {&work.seq, &work.first, &work.part, &work.range, &work.q.start, &work.q.len, &work.q.before,
+                 &work.q.poison})
+    *x = __builtin_amdgcn_readfirstlane(*x);       // equal in every lane: into scalar registers
   if (item == 0 && threadIdx.x == 0 && p.range != nullptr) *p.range = work.range;
   if (work.seq < 0) return;
   const int b = work.seq;

@@ -270,6 +270,31 @@ def test_prefill_many_tiles(gpu):
     check_attention(out, lse, prefill_reference(c))
 
 
+def test_prefill_hundreds_of_requests(gpu):
+    """More requests than a workgroup has threads: tiles of 1 to 128 steps in order of length, one request
+    with a context that no table holds, another without rows; and few rows in all, whose keys are cut."""
+    lens = [1 + 7 * b % 5 for b in range(600)]
+    ctx = [61 * b % 257 for b in range(600)]
+    lens[3], lens[299], ctx[299], ctx[411], lens[599] = 0, 75, 130, 8100, 140
+    c = prefill_case(37, 2, 1, lens, ctx, sharp=2.0)
+    ref = prefill_reference(c)
+    c["ctx"][298] = c["table"].shape[1] * 16
+    at = sum(lens[:298])
+    for x in ref:
+        x[at:at + lens[298]] = np.nan
+    check_attention(*run_prefill(c), ref)
+    c = prefill_case(38, 1, 1, [1 + (b == 280) for b in range(300)], [4000 if b == 280 else b for b in range(300)])
+    check_attention(*run_prefill(c), prefill_reference(c))
+
+
+def test_prefill_hundreds_of_row_ranges_out_of_order_stay_in_bounds(gpu):
+    c = prefill_case(39, 2, 1, [3] * 300, [b % 70 for b in range(300)])
+    c["cu"] = ints(np.random.default_rng(6).integers(-5, 905, 301))
+    out, _ = run_prefill(c)
+    torch.cuda.synchronize()
+    assert out.shape == (900, 2, 128)
+
+
 def test_prefill_long_prompt(gpu):
     """Several hundred workgroups, one request: rows of every tile against fp64 (on the GPU, in torch)."""
     gen = torch.Generator().manual_seed(23)
