@@ -286,9 +286,8 @@ constexpr int64_t kMaxGrid = (1 << 24) - 1;
 // Work items of a KV head: its row tiles, or, where there are fewer than the chip keeps resident (two
 // workgroups a compute unit), as many as that, the tiles' keys being cut into ranges.  `entries` is the most
 // that one tile's may be cut into: what the items leave room for beside the other tiles, the
-// steps of a full table, kMostEntries, and kPairBytes of pairs (4 ranges at least).
+// steps of a full table, and kPairBytes of pairs (4 ranges at least).
 constexpr int64_t kRowsResident = 512;
-constexpr int64_t kMostEntries = 64;
 constexpr int64_t kPairBytes = 128 << 20;
 struct Items {
   int64_t slots = 0, entries = 1;
@@ -305,7 +304,7 @@ Items rows_items(int64_t rows, int64_t hq, int64_t hkv, int64_t seqs, int64_t ma
   if (direct && qf::kRowsAloneUs * (float)steps <=
                     qf::kRowsStepUs + qf::kRowsJoinUs + 0.5f * qf::kRowsPairUs * (float)(rows * hq))
     return it;
-  it.entries = std::max<int64_t>(1, std::min({kRowsResident / hkv - full + 1, steps, kMostEntries,
+  it.entries = std::max<int64_t>(1, std::min({kRowsResident / hkv - full + 1, steps,
                                               std::max<int64_t>(4, in_bytes)}));
   if (it.entries > 1) it.slots = kRowsResident / hkv;
   return it;

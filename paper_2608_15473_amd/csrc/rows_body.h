@@ -59,10 +59,23 @@ constexpr float kFar = 1048576.0f;       // log2 units
 // Measured (us, cut to fill the chip / uncut): 1,024 causal tokens at 16/8 heads 32.8 / 24.2, 2,048 54.7 /
 // 44.1, 128 11.4 / 8.4, but 256 tokens after 4,096 32.2 / 81; 32 rows over 8,192 positions at 32/8 heads
 // 14.6 with 4 steps a range, 16.6 with 3.
+// Beside the sweep (no out) fewer items leave it room: half or all of the compute units without one, or half of
+// what they hold, as long as the ranges stay short.  Whole calls with a quarter / half / all of the items, us:
+// 32 requests over 8,192 positions at 32/8 heads (ranges of 9 / 5 / 5 steps) 26.6 / 31.8 / 32.7, 64 over 16,384
+// (37 / 18 / 10) 61.0 / 56.2 / 64.7, 256 in 8 groups over up to 4,096 (64 / 22 / 10) 104.6 / 90.9 / 100.2, but
+// 4 over 1,531 (2 / 1 / 1) 13.2 / 12.0 / 12.5 and 128 in 3 groups over up to 32,768 at 64/8 (-/ 126 / 53)
+// 481 / 222 / 206-211.
 __device__ __forceinline__ int range_of(const RowsParams& p, int64_t all, int64_t tiles, int longest) {
   if (tiles == 0) return 1;
-  const int64_t room = p.slots - tiles;
-  int64_t least = room > 0 ? (all + room - 1) / room : INT32_MAX;
+  auto fits = [&](int64_t slots) {       // steps of a range with at most so many items
+    return slots > tiles ? (all + slots - tiles - 1) / (slots - tiles) : (int64_t)INT32_MAX;
+  };
+  int64_t least = fits(p.slots);
+  if (p.out == nullptr) {
+    const int64_t quarter = fits(p.slots / 4), half = fits(p.slots / 2);
+    if (quarter >= 4 && quarter <= 12) least = quarter;
+    else if (half >= 4 && half <= 32) least = half;
+  }
   least = max(least, (int64_t)((longest + p.entries - 1) / p.entries));
   const float avg = (float)all / (float)tiles, pair = kRowsPairUs * (float)p.rows * (float)p.hq;
   const int64_t range = max(least, (int64_t)ceilf(sqrtf(pair * avg / kRowsStepUs)));

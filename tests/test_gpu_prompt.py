@@ -142,6 +142,11 @@ ROPE = [
 ]
 
 
+ROPE += [
+    dict(hq=1, hkv=1, lens=[0] * 3 + [b % 3 for b in range(130)] + [0] * 70 + [2], ctx=[7 * b % 50 for b in range(204)]),
+]
+
+
 @pytest.mark.parametrize("kw", ROPE, ids=range(len(ROPE)))
 def test_rope_append(gpu, kw):
     c = rope_case(11, **kw)
@@ -249,6 +254,7 @@ PREFILL += [
     dict(hq=4, hkv=2, lens=[3, 0, 40], ctx=[2, 0, 6000], sharp=2.0),     # one tile cut, others not
     dict(hq=1, hkv=1, lens=[1 + b % 2 for b in range(100)], ctx=[3000 if b == 77 else b for b in range(100)]),
     dict(hq=32, hkv=4, lens=[33], ctx=[2500], sharp=2.0),                # full tiles, cut
+    dict(hq=8, hkv=1, lens=[1], ctx=[13000], sharp=2.0),                 # hundreds of ranges
 ]
 
 
@@ -293,6 +299,28 @@ def test_prefill_hundreds_of_row_ranges_out_of_order_stay_in_bounds(gpu):
     out, _ = run_prefill(c)
     torch.cuda.synchronize()
     assert out.shape == (900, 2, 128)
+
+
+def test_pages_past_four_gibibytes(gpu):
+    """A pool of which K alone is 5 GB, the pages at its end: appended to, read by prefill and as a prefix."""
+    pages = 1_220_000
+    c = prefill_case(40, 4, 1, [9, 40], [70, 0], garbage=False)
+    d = {k: v.to(DEV) if isinstance(v, torch.Tensor) else v for k, v in c.items()}
+    small = d["kc"].shape[0]
+    far = dict(d, table=torch.where(d["table"] >= 0, d["table"] + (pages - small), d["table"]))
+    for x in ("kc", "vc"):
+        far[x] = torch.empty(pages, 1, 16, 128, dtype=torch.bfloat16, device=DEV)
+        far[x][-small:] = d[x]
+    new = torch.randn(49, 1, 128, generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    res = []
+    for e in (d, far):
+        qf.qkv_rope_append(None, new, new, e["kc"], e["vc"], e["table"], e["ctx"], e["cu"])
+        res.append(qf.attn_prefill(e["q"], e["kc"], e["vc"], e["table"], e["ctx"], e["cu"]))
+        res.append(qf.attn_decode_shared(e["q"][:2], e["kc"], e["vc"], e["table"][:1], e["ctx"][:1],
+                                         ints([0, 2]).to(DEV), e["table"][1:].repeat(2, 1),
+                                         ints([40, 3]).to(DEV), 1))
+    for a, b in zip(res[0] + res[1], res[2] + res[3]):
+        assert bool(torch.isfinite(a.float()).all()) and torch.equal(a, b)
 
 
 def test_prefill_long_prompt(gpu):
