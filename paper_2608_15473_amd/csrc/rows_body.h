@@ -154,17 +154,30 @@ __device__ __forceinline__ int tiles_of(const Sequence& q, int gshift) {
 // A tile's keys are cut into ranges of `range` steps.
 __device__ __forceinline__ int ranges_of(int steps, int range) { return steps > 0 ? (steps - 1) / range + 1 : 1; }
 
-// Sum and maximum over the lanes, in scalar registers.
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+// x combined over the lanes up to this one, six steps of DPP: rows of 16 first, then rows into later ones (a
+// reduction by shuffles takes some 800 cycles through LDS, and a bisection below has ten).  `none`: of lanes that
+// a step finds nothing for.
+template <typename F>
+__device__ __forceinline__ int upto(int x, int none, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));      // row_shr:1, 2, 4, 8
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));      // row_bcast:15
+  return f(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));   // row_bcast:31
+}
+__device__ __forceinline__ int upto_sum(int x) {
+  return upto(x, 0, [](int a, int b) { return a + b; });
+}
+// Over all lanes, in a scalar register.
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(upto_sum(x), 63); }
+__device__ __forceinline__ int wave_max(int x) {
+  return __builtin_amdgcn_readlane(upto(x, INT32_MIN, [](int a, int b) { return max(a, b); }), 63);
+}
+__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  const uint32_t high = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-  return (int64_t)((uint64_t)high << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
-}
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
+  return x;
 }
 
 // What a workgroup does: rows first .. first + 127 of sequence seq, key range `part`.
@@ -180,16 +193,6 @@ __device__ __forceinline__ int tiles_from(const Sequence& q, int gshift, int til
   if (need >= q.len) return 0;
   return tiles - (int)((need << gshift) / kRowsTile);
 }
-// Running sum over the lanes, this one's included.
-__device__ __forceinline__ int64_t upto_sum(int64_t x) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if ((int)(threadIdx.x & 63) >= o) x += y;
-  }
-  return x;
-}
-
 // Work item `slot` of a KV head.  The range (range_of) leaves at most p.slots items and p.entries ranges a
 // tile: with t tiles of n steps each sequence has t ceil(n / range) of them.  Items of a range of keys lie
 // side by side (their tiles read the same keys).  Causal tiles without ranges differ in length: they are taken
@@ -204,30 +207,30 @@ __device__ __forceinline__ Work find_among_few(const RowsParams& p, int gshift, 
   const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
   const bool by_length = p.entries == 1 && p.causal;
   int range = INT32_MAX, above = 0;      // above: tiles of the sequence that are longer
-  int64_t before = 0, items;
+  int before = 0, items;                 // at most 64 x 2^24 tiles; ranges only of few
   if (by_length) {
     int low = 0, high = wave_max(n) + 1; // tiles of at least low, high steps: > slot (or none), <= slot
     while (high - low > 1) {
       const int mid = (low + high) / 2;
-      if (wave_sum((int64_t)tiles_from(q, gshift, t, mid)) > slot) low = mid; else high = mid;
+      if (wave_sum(tiles_from(q, gshift, t, mid)) > slot) low = mid; else high = mid;
     }
     above = tiles_from(q, gshift, t, low + 1);
     before = wave_sum(above);
     items = tiles_from(q, gshift, t, low) - above;
   } else {
     if (p.entries > 1) {
-      const int64_t all = wave_sum((int64_t)t * n), tiles = wave_sum(t);
-      const int longest = wave_max(n);
+      const int64_t all = wave_sum64((int64_t)t * n);
+      const int tiles = wave_sum(t), longest = wave_max(n);
       range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
     }
-    items = (int64_t)t * ranges_of(n, range);
+    items = t * ranges_of(n, range);
   }
-  const int64_t upto = before + upto_sum(items);
-  const uint64_t past = __ballot(upto > slot);
+  const int end = before + upto_sum(items);
+  const uint64_t past = __ballot(end > slot);
   if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
   const int l = __builtin_ctzll(past);
   auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-  const int i = __builtin_amdgcn_readfirstlane(slot - (int)__shfl(upto - items, l)), tl = of(t);
+  const int i = __builtin_amdgcn_readfirstlane(slot - of(end - items)), tl = of(t);
   const Sequence found{of(q.start), of(q.len), of(q.before), of(q.poison)};
   if (by_length) return Work{l, (tl - of(above) - 1 - i) * kRowsTile, 0, range, found};
   return Work{l, i % tl * kRowsTile, i / tl, range, found};
@@ -271,13 +274,12 @@ __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift,
       }
     });
     __syncthreads();
-    const int64_t items = lane < 33 ? lds.tiles_of_bits[32 - lane] : 0;
-    const int64_t upto = upto_sum(items);
-    const uint64_t past = __ballot(upto > slot);
+    const int items = lane < 33 ? lds.tiles_of_bits[32 - lane] : 0, end = upto_sum(items);
+    const uint64_t past = __ballot(end > slot);
     if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
     const int l = __builtin_ctzll(past);
     bits = __builtin_amdgcn_readfirstlane(32 - l);
-    before = __shfl(upto - items, l);
+    before = __builtin_amdgcn_readlane(end - items, l);
   } else if (p.entries > 1) {
     int64_t all = 0, tiles = 0;
     int longest = 0;
@@ -286,8 +288,8 @@ __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift,
       tiles += t;
       longest = max(longest, n);
     });
-    all = wave_sum(all);
-    tiles = wave_sum(tiles);
+    all = wave_sum64(all);
+    tiles = wave_sum64(tiles);
     longest = wave_max(longest);
     if (lane == 0) {
       lds.all[wave] = all;
@@ -309,7 +311,9 @@ __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift,
   };
   int64_t mine = 0;
   each([&](int, const Sequence& q, int t, int n) { mine += items_of(q, t, n); });
-  int64_t upto = upto_sum(mine);
+  // No call has 2^24 items; more, of ranges of rows that overlap, must not wrap to two owners of a slot.
+  mine = min(mine, (int64_t)1 << 24);
+  int64_t upto = upto_sum((int)mine);
   __syncthreads();                       // the sums above are read
   if (lane == 63) lds.all[wave] = upto;
   __syncthreads();
