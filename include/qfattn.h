@@ -513,7 +513,8 @@ int qf_qkv_rope_append(const qf_decode_desc* desc, int32_t n_tokens, const int32
  *   ctx_lens    int32 [batch], with ctx_lens[b] + its tokens <= max_pages_per_seq * P; otherwise the
  *               request's out and lse are NaN.  A page outside the pool makes NaN of the rows that see it.
  *   cu_tokens   int32 [batch + 1], not decreasing, in [0, n_tokens].  Rows that lie in no request are
- *               left as they are.
+ *               left as they are.  Values out of order or range never cause an out-of-bounds access, but
+ *               leave the outputs unspecified.
  *   out         bf16 [n_tokens, Hq, D], 8-byte aligned; lse fp32 [n_tokens, Hq] natural log, or NULL.
  *               Neither may overlap the inputs.
  *   workspace   at least qf_attn_prefill_workspace_size() bytes, 16-byte aligned; may be NULL when that
@@ -538,7 +539,8 @@ int qf_attn_prefill(const qf_decode_desc* desc, int32_t n_tokens, const void* q,
  *   desc ... n_shards   as for qf_attn_decode_split (max_shards and n_shards: of a request's own
  *               positions).  A request may have no position of its own.
  *   n_groups    >= 0; with 0 the three arrays may be NULL.
- *   group_rows  int32 [n_groups + 1], not decreasing, in [0, batch].
+ *   group_rows  int32 [n_groups + 1], not decreasing, in [0, batch].  Values out of order or range never
+ *               cause an out-of-bounds access, but leave the outputs unspecified.
  *   prefix_lens int32 [n_groups], 0 <= n <= max_prefix_pages * P; otherwise, and where a page lies
  *               outside the pool, the group's out and lse are NaN.
  *   prefix_table   int32 [n_groups, max_prefix_pages], pages of the same pools.

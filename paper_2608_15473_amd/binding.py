@@ -703,7 +703,7 @@ def _same_device(device, **tensors):
             raise QFError(QF_EINVAL, f"{name} is on {t.device}, not on {device}")
 
 
-def _cache_of(k_cache, v_cache, block_table, ctx_lens):
+def _cache_of(k_cache, v_cache, block_table, ctx_lens, max_pages=None):
     """Checks of a paged cache and its indexes; returns (batch, Hkv, P, D)."""
     _require(k_cache, "k_cache", torch.bfloat16, 4)
     _require(v_cache, "v_cache", torch.bfloat16, 4)
@@ -715,6 +715,8 @@ def _cache_of(k_cache, v_cache, block_table, ctx_lens):
         _require(block_table, "block_table", torch.int32, 2)
         if block_table.shape[0] != B:
             raise QFError(QF_EINVAL, f"block_table has {block_table.shape[0]} rows for {B} requests")
+        if max_pages is not None and max_pages != block_table.shape[1]:
+            raise QFError(QF_EINVAL, f"block_table has {block_table.shape[1]} pages a row, not {max_pages}")
     return (B, *k_cache.shape[1:])
 
 
@@ -760,7 +762,7 @@ class RopeAppendPlan(_Plan):
         T, _, D = some.shape
         strides = [0 if t is None else _heads_of(t, name, T) for t, name in ((q, "q"), (k, "k"), (v, "v"))]
         if k is not None:
-            B, Hkv, P, Dc = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+            B, Hkv, P, Dc = _cache_of(k_cache, v_cache, block_table, ctx_lens, max_pages)
             if tuple(k.shape) != (T, Hkv, Dc) or tuple(v.shape) != (T, Hkv, Dc):
                 raise QFError(QF_EINVAL, "k and v do not match the cache")
             if max_pages is None:
@@ -882,7 +884,7 @@ class PrefillPlan(_Plan):
     def __init__(self, q, k_cache, v_cache, block_table, ctx_lens, cu_tokens, scale=None, out=None,
                  lse=None, workspace=None, max_pages=None, want_lse=True, stream=None):
         _require(q, "q", torch.bfloat16, 3)
-        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens, max_pages)
         _require(cu_tokens, "cu_tokens", torch.int32, 1)
         if cu_tokens.shape[0] != B + 1:
             raise QFError(QF_EINVAL, f"cu_tokens must have {B + 1} entries")
@@ -936,7 +938,7 @@ class SharedDecodePlan(_Plan):
                  n_shards, max_shards=None, scale=None, out=None, lse=None, workspace=None,
                  max_pages=None, want_lse=True, pair=False, stream=None):
         _require(q, "q", torch.bfloat16, 3)
-        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens)
+        B, Hkv, P, D = _cache_of(k_cache, v_cache, block_table, ctx_lens, max_pages)
         if q.shape[0] != B or q.shape[2] != D:
             raise QFError(QF_EINVAL, "q does not match ctx_lens and the cache")
         _require(prefix_table, "prefix_table", torch.int32, 2)

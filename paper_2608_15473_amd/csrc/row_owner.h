@@ -12,8 +12,9 @@ struct RowOwner {
 
 // The sequence that row t of `rows` lies in, by a whole wavefront (every lane gets the answer): as cu
 // does not decrease, it is the last one that starts at or before t, found 64 starts at a time (of 4,096
-// sequences in two rounds: a step of 4,096 requests of 48 heads with cu 61 -> 27 us).  Values that are out of range or out of order give no sequence or another one,
-// never an index outside [0, seqs).  cu == null: one row each.
+// sequences in two rounds: norm, rotation and append of so many requests' single tokens of 48 heads 61 ->
+// 27 us).  Values that are out of range or out of order give no sequence or another one, never an index
+// outside [0, seqs).  cu == null: one row each.
 __device__ __forceinline__ RowOwner row_owner(const int32_t* __restrict__ cu, int32_t seqs,
                                               int32_t rows, int32_t t) {
   if (cu == nullptr) return RowOwner{t < seqs ? t : -1, 0};

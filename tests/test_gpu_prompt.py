@@ -143,7 +143,8 @@ ROPE = [
 
 
 ROPE += [
-    dict(hq=1, hkv=1, lens=[0] * 3 + [b % 3 for b in range(130)] + [0] * 70 + [2], ctx=[7 * b % 50 for b in range(204)]),
+    dict(hq=1, hkv=1, lens=[0] * 3 + [b % 3 for b in range(130)] + [0] * 70 + [2],
+         ctx=[7 * b % 50 for b in range(204)]),
 ]
 
 
@@ -428,6 +429,21 @@ def test_prefill_row_ranges_out_of_order_stay_in_bounds(gpu):
         if cu == [3, 5, 5, 9]:
             assert bool((out[:3] == 7.0).all()) and bool((out[9:] == 7.0).all())
             assert not bool((out[3:9] == 7.0).all())
+
+
+def test_a_table_has_the_pages_that_are_named(gpu):
+    c = prefill_case(30, 4, 1, [2], [20])
+    d = {k: v.to(DEV) if isinstance(v, torch.Tensor) else v for k, v in c.items()}
+    wrong = d["table"].shape[1] + 1
+    cache = (d["kc"], d["vc"], d["table"], d["ctx"])
+    q = d["q"][:1]
+    with pytest.raises(qf.QFError, match="pages a row"):
+        qf.attn_prefill(d["q"], *cache, d["cu"], max_pages=wrong)
+    with pytest.raises(qf.QFError, match="pages a row"):
+        qf.qkv_rope_append(q, q[:, :1], q[:, :1], *cache, max_pages=wrong)
+    with pytest.raises(qf.QFError, match="pages a row"):
+        qf.attn_decode_shared(q, d["kc"], d["vc"], d["table"], d["ctx"], ints([0, 1]).to(DEV), d["table"],
+                              d["ctx"], 1, max_pages=wrong)
 
 
 def test_prefill_identity_table_and_no_lse(gpu):
