@@ -171,6 +171,7 @@ struct RowsParams {
 };
 constexpr int kRowsTile = 128;  // query rows (tokens x query heads of a KV head) of a workgroup
 constexpr int kKeyTile = 64;    // positions of a step
+constexpr int kRowsResident = 512;   // workgroups that the chip keeps, two a compute unit
 // What key ranges cost and save, us (rows_body.h: range_of).
 constexpr float kRowsAloneUs = 1.2f, kRowsStepUs = 2.0f, kRowsJoinUs = 8.0f, kRowsPairUs = 3.44e-4f;
 // Every sequence has at most one tile that is not full.

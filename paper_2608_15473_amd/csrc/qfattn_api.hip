@@ -284,10 +284,9 @@ int finish_split(const Split& sp, hipStream_t s) {
 constexpr int64_t kMaxGrid = (1 << 24) - 1;
 
 // Work items of a KV head: its row tiles, or, where there are fewer than the chip keeps resident (two
-// workgroups a compute unit), as many as that, the tiles' keys being cut into ranges.  `entries` is the most
+// workgroups a compute unit, kRowsResident), as many as that, the tiles' keys being cut into ranges.  `entries` is the most
 // that one tile's may be cut into: what the items leave room for beside the other tiles, the
 // steps of a full table, and kPairBytes of pairs (4 ranges at least).
-constexpr int64_t kRowsResident = 512;
 constexpr int64_t kPairBytes = 128 << 20;
 struct Items {
   int64_t slots = 0, entries = 1;
@@ -300,13 +299,13 @@ Items rows_items(int64_t rows, int64_t hq, int64_t hkv, int64_t seqs, int64_t ma
   const int64_t in_bytes = kPairBytes / (rows * hq * (qf::kHeadDim + 1) * (int64_t)sizeof(float));
   Items it;
   it.slots = qf::rows_tiles(rows, hq / hkv, seqs);
-  if (it.slots >= kRowsResident / hkv) return it;
+  if (it.slots >= qf::kRowsResident / hkv) return it;
   if (direct && qf::kRowsAloneUs * (float)steps <=
                     qf::kRowsStepUs + qf::kRowsJoinUs + 0.5f * qf::kRowsPairUs * (float)(rows * hq))
     return it;
-  it.entries = std::max<int64_t>(1, std::min({kRowsResident / hkv - full + 1, steps,
+  it.entries = std::max<int64_t>(1, std::min({qf::kRowsResident / hkv - full + 1, steps,
                                               std::max<int64_t>(4, in_bytes)}));
-  if (it.entries > 1) it.slots = kRowsResident / hkv;
+  if (it.entries > 1) it.slots = qf::kRowsResident / hkv;
   return it;
 }
 

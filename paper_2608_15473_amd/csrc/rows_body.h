@@ -203,11 +203,21 @@ __device__ __forceinline__ int tiles_from(const Sequence& q, int gshift, int til
   if (need >= q.len) return 0;
   return tiles - (int)((need << gshift) / kRowsTile);
 }
+// The place among the tiles by length, the longest first, that slot takes.  A workgroup that starts late has to be
+// short; and of the two that begin on a compute unit, the slot-th and the one `half` after it, one is as much
+// longer than the middle as the other is shorter: the first half of the places go in reverse (one prompt, longest
+// first in both halves -> so, us: 1,500 tokens at 32/8 heads 45.5 -> 40.1, 2,048 51.8 -> 49.4, 4,096 148 -> 142,
+// 3,000 at 16/8 72 -> 66.5; from some thousand tiles on no difference).
+__device__ __forceinline__ int length_rank(const RowsParams& p, int slot) {
+  const int half = min(kRowsResident / 2 / p.hkv, p.slots);
+  return slot < half ? half - 1 - slot : slot;
+}
+
 // Work item `slot` of a KV head.  The range (range_of) leaves at most p.slots items and p.entries ranges a
 // tile: with t tiles of n steps each sequence has t ceil(n / range) of them.  Items of a range of keys lie
 // side by side (their tiles read the same keys).  Causal tiles without ranges differ in length: they are taken
-// the longest first (a workgroup that starts late has to be short), by bisection for the slot-th tile's number
-// of steps, then among the tiles of just that many.
+// by length (length_rank), found by bisection for the tile's number of steps, then among the tiles of just that
+// many.
 // At most 64 sequences: every wavefront finds it for itself, a lane to a sequence.
 __device__ __forceinline__ Work find_among_few(const RowsParams& p, int gshift, int slot) {
   const int lane = threadIdx.x & 63;
@@ -215,10 +225,16 @@ __device__ __forceinline__ Work find_among_few(const RowsParams& p, int gshift, 
   if (lane < p.seqs) q = sequence(p.cu, p.ctx_lens, p.rows, p.max_pages, p.causal, lane);
   const int t = tiles_of(q, gshift);
   const int n = t > 0 ? steps_of(sees_of(q, p.causal, q.len - 1)) : 0;
-  const bool by_length = p.entries == 1 && p.causal;
   int range = INT32_MAX, above = 0;      // above: tiles of the sequence that are longer
+  if (p.entries > 1) {
+    const int64_t all = wave_sum64((int64_t)t * n);
+    const int tiles = wave_sum(t), longest = wave_max(n);
+    range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
+  }
+  const bool by_length = p.causal && range == INT32_MAX;
   int before = 0, items;                 // at most 64 x 2^24 tiles; ranges only of few
   if (by_length) {
+    slot = length_rank(p, slot);
     int low = 0, high = wave_max(n) + 1; // tiles of at least low, high steps: > slot (or none), <= slot
     while (high - low > 1) {
       const int mid = (low + high) / 2;
@@ -228,11 +244,6 @@ __device__ __forceinline__ Work find_among_few(const RowsParams& p, int gshift, 
     before = wave_sum(above);
     items = tiles_from(q, gshift, t, low) - above;
   } else {
-    if (p.entries > 1) {
-      const int64_t all = wave_sum64((int64_t)t * n);
-      const int tiles = wave_sum(t), longest = wave_max(n);
-      range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
-    }
     items = t * ranges_of(n, range);
   }
   const int end = before + upto_sum(items);
@@ -257,7 +268,6 @@ struct Many {
 };
 __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift, int slot, Many& lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool by_length = p.entries == 1 && p.causal;
   int range = INT32_MAX, bits = 0;
   int64_t before = 0;
   auto each = [&](auto use) {            // this thread's sequences: their tiles, and steps of the longest
@@ -272,25 +282,7 @@ __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift,
     return k > 31 ? 0 : tiles_from(q, gshift, t, k == 0 ? 0 : 1 << (k - 1));
   };
   if (threadIdx.x == 0) lds.work = Work{-1, 0, 0, 0, Sequence{0, 0, 0, 0}};
-  if (by_length) {
-    if (threadIdx.x < 33) lds.tiles_of_bits[threadIdx.x] = 0;
-    __syncthreads();
-    each([&](int, const Sequence& q, int t, int n) {
-      int longer = 0;
-      for (int k = n > 0 ? 32 - __builtin_clz(n) : 0; longer < t && k >= 0; --k) {
-        const int so_far = with_bits(q, t, k);
-        if (so_far > longer) atomicAdd(&lds.tiles_of_bits[k], so_far - longer);
-        longer = so_far;
-      }
-    });
-    __syncthreads();
-    const int items = lane < 33 ? lds.tiles_of_bits[32 - lane] : 0, end = upto_sum(items);
-    const uint64_t past = __ballot(end > slot);
-    if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
-    const int l = __builtin_ctzll(past);
-    bits = __builtin_amdgcn_readfirstlane(32 - l);
-    before = __builtin_amdgcn_readlane(end - items, l);
-  } else if (p.entries > 1) {
+  if (p.entries > 1) {
     int64_t all = 0, tiles = 0;
     int longest = 0;
     each([&](int, const Sequence&, int t, int n) {
@@ -314,6 +306,27 @@ __device__ __forceinline__ Work find_among_many(const RowsParams& p, int gshift,
       longest = max(longest, lds.longest[w]);
     }
     range = __builtin_amdgcn_readfirstlane(range_of(p, all, tiles, longest));
+  }
+  const bool by_length = p.causal && range == INT32_MAX;
+  if (by_length) {
+    slot = length_rank(p, slot);
+    if (threadIdx.x < 33) lds.tiles_of_bits[threadIdx.x] = 0;
+    __syncthreads();
+    each([&](int, const Sequence& q, int t, int n) {
+      int longer = 0;
+      for (int k = n > 0 ? 32 - __builtin_clz(n) : 0; longer < t && k >= 0; --k) {
+        const int so_far = with_bits(q, t, k);
+        if (so_far > longer) atomicAdd(&lds.tiles_of_bits[k], so_far - longer);
+        longer = so_far;
+      }
+    });
+    __syncthreads();
+    const int items = lane < 33 ? lds.tiles_of_bits[32 - lane] : 0, end = upto_sum(items);
+    const uint64_t past = __ballot(end > slot);
+    if (past == 0) return Work{-1, 0, 0, range, Sequence{0, 0, 0, 0}};
+    const int l = __builtin_ctzll(past);
+    bits = __builtin_amdgcn_readfirstlane(32 - l);
+    before = __builtin_amdgcn_readlane(end - items, l);
   }
   auto items_of = [&](const Sequence& q, int t, int n) {
     return by_length ? (int64_t)(with_bits(q, t, bits) - with_bits(q, t, bits + 1))
@@ -358,9 +371,12 @@ __device__ __forceinline__ Work find_work(const RowsParams& p, int gshift, int s
   int range = INT32_MAX;
   if (p.entries > 1) range = __builtin_amdgcn_readfirstlane(range_of(p, (int64_t)t * n, t, n));
   const int parts = ranges_of(n, range);
+  if (p.causal && range == INT32_MAX) {
+    const int rank = length_rank(p, slot);
+    return Work{rank < t ? 0 : -1, (t - 1 - rank) * kRowsTile, 0, range, q};
+  }
   if (slot >= t * parts) return Work{-1, 0, 0, range, q};
-  const int i = p.entries > 1 ? slot : t - 1 - slot;
-  return Work{0, i % t * kRowsTile, i / t, range, q};
+  return Work{0, slot % t * kRowsTile, slot / t, range, q};
 }
 
 // A bf16 pair with zeros for infinities and NaN.
