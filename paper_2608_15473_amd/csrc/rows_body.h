@@ -525,9 +525,10 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
 
   // From step `edge` on, some row of the tile does not see every key.  A masked key's weight is 0, but 0
   // times an infinity or NaN is not: so every wavefront makes zeros of those in its page of V.  Where there
-  // were any (rare), they are added at the end to the rows that do see them.
+  // were any at a position of the request's (rare; what lies behind its last in the page is nobody's), they are
+  // added at the end to the rows that do see them.
   const int edge = max(k0, sees_of(seq, p.causal, work.first >> gshift) / kKeyTile);
-  auto clean = [&](int buffer) {
+  auto clean = [&](int kt, int buffer) {
     unsigned char* const mine = s_kv + buffer + kTileBytes + wave * (P * D * 2);
     u32x4 x[4];
 #pragma unroll
@@ -537,7 +538,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
       const u32x4 y = {finite_pair(x[j].x), finite_pair(x[j].y), finite_pair(x[j].z), finite_pair(x[j].w)};
       if (((x[j].x ^ y.x) | (x[j].y ^ y.y) | (x[j].z ^ y.z) | (x[j].w ^ y.w)) != 0) {
         reinterpret_cast<u32x4*>(mine)[64 * j + lane] = y;
-        s_found = 1;
+        if (kt * kKeyTile + wave * P + 4 * j + (lane >> 4) < keys) s_found = 1;
       }
     }
     __syncthreads();
@@ -715,7 +716,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
         load_k(page, to);
         next = entries(kt + 3);
       }
-      if (kt >= edge) clean(to);
+      if (kt >= edge) clean(kt, to);
       bf16x8 ring[kRing];
 #pragma unroll
       for (int i = 0; i < kRing - 1; ++i) ring[i] = fragment(0, i);
@@ -732,7 +733,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
       to ^= kBufferBytes;
     }
     arrived();
-    if (kt >= edge) clean(to);
+    if (kt >= edge) clean(kt, to);
     weigh_all(s, now);
 #pragma unroll
     for (int i = 8; i < 16; ++i) product_part(fragment(0, i), i, w);
@@ -741,7 +742,7 @@ __device__ __forceinline__ void item(const RowsParams& p, const unsigned item, L
 
     if (s_found != 0) {                              // infinities and NaN among the keys from `edge` on
 #pragma unroll 1
-      for (int pos = edge * kKeyTile; pos < min(keys, k1 * kKeyTile); ++pos) {
+      for (int pos = edge * kKeyTile; pos < (int)min((int64_t)keys, (int64_t)k1 * kKeyTile); ++pos) {
         const int entry = bt ? bt[pos / P] : b * p.max_pages + pos / P;
         if ((unsigned)entry >= (unsigned)p.num_pages) continue;    // its scores are NaN
         const uint16_t* const x = p.v + entry * page_stride + head_off + (pos % P) * D + 4 * half;
