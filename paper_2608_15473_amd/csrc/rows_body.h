@@ -18,7 +18,7 @@
 // transposed by ds_read_b64_tr_b16.  Rounding the weights to bf16 (2^-9 relative, to nearest, so errors
 // average out over the keys) is what the matrix cores take; l sums the unrounded weights in fp32.
 //
-// A compute unit holds two workgroups (64 KB of LDS each for two steps' keys, 204 registers): one wavefront
+// A compute unit holds two workgroups (64 KB of LDS each for two steps' keys, 206 registers): one wavefront
 // issues a vector instruction every 8 cycles at most, so two a SIMD are what it takes to weigh scores under the
 // matrix instructions.  Measured: 4,096 tokens after 12,288 at 64/8 heads 1.73 to 1.81 ms, 1.07 to 1.11 PFLOP/s,
 // the matrix cores busy 59% of the cycles and the vector ALUs 55%, at the 1.73 GHz that the power limit leaves
